@@ -227,10 +227,12 @@ def _plain_route(S, k):
                 slots=slots.view(T, k).to(i32), offsets=offsets.to(i32))
 
 
-def _plain_dispatch(x, perm, k, into):
+def _plain_dispatch(x, slots, into):
     out = into.clone()
-    src = torch.where(perm < 0, 0, perm.long() // k)
-    return torch.where((perm >= 0)[:, None], x[src], out)
+    for j in range(slots.shape[1]):
+        sel = slots[:, j] >= 0
+        out[slots[sel, j].long()] = x[sel]
+    return out
 
 
 def _plain_combine(F, slots, w, residual):
@@ -324,7 +326,7 @@ def _plain(st):
     if case["kind"] == "route":
         return _plain_route(st["S"], case["k"])
     if case["kind"] == "move":
-        X = _plain_dispatch(st["x"], st["perm"], case["k"], st["X"])
+        X = _plain_dispatch(st["x"], st["slots"], st["X"])
         Y = _plain_combine(st["F"], st["slots"], st["w"], st["x"])
         dF, dw = _plain_combine_backward(st["dY"], st["F"], st["slots"], st["w"], st["dF"])
         return dict(X=X, Y=Y, dF=dF, dw=dw,
@@ -345,7 +347,7 @@ def run(st):
         return dict(assign=r.assign, scores=r.scores, perm=r.perm, slots=r.slots,
                     offsets=r.offsets)
     if kind == "move":
-        X = pb.dispatch(st["x"], st["perm"], case["k"], out=st["X"])
+        X = pb.dispatch(st["x"], st["slots"], out=st["X"])
         Y = pb.combine(st["F"], st["slots"], weights=st["w"], residual=st["x"])
         dF, dw = pb.combine_backward(st["dY"], st["F"], st["slots"], st["w"], out=st["dF"])
         dx = pb.combine(st["dX"], st["slots"], residual=st["dY"])
