@@ -445,6 +445,150 @@ int base_gate_backward(const void *dY, const void *F, const void *H, const void 
                        int64_t T, int64_t E, int64_t d, int dtype, void *stream);
 
 /* ------------------------------------------------------------------------ */
+/* k experts a token, and the experts themselves                             */
+/* ------------------------------------------------------------------------ */
+/*
+ * The layers the paper compares with send a token to k experts (Sec. 4.2: two
+ * in the sparsely gated mixture); an expert is a stack of residual feed-forward
+ * blocks (Sec. 3.1): layer norm, projection, ReLU, projection back. The calls below
+ * route with k experts, move rows there and back, and compute the blocks and
+ * their gradients on routed rows.
+ *
+ * Pair p = t k + j is choice j of token t; N = T k. The routed order lists the
+ * pairs expert after expert, in ascending order within one. perm [N] holds the
+ * pair of each routed row, slots [T, k] the routed row of each pair, offsets
+ * [E + 1] the experts' row ranges: expert e's rows are [offsets[e], offsets[e + 1]).
+ * A pair without an expert has slot -1 and no row; the rows of perm behind
+ * offsets[E] are then -1. Buffers over routed rows have N rows always, so no
+ * call waits for the counts, and rows behind offsets[E] are neither read as
+ * input that matters nor written.
+ * T k < 2^31, E <= 2048, k <= 64 (and k <= E for base_topk_assign).
+ *
+ * base_topk_assign - the k highest-scoring experts of each token, highest first,
+ * the lowest index on ties; then the sort. A score of -inf or NaN is never
+ * chosen: a mask of -inf forbids experts, and a row of them (padding) has no
+ * expert at all.
+ *   S         [device] T x E float32 scores, 16-byte aligned
+ *   assign    [device] int32 [T, k] out, -1 where fewer than k experts are allowed
+ *   scores    [device] float32 [T, k] out, may be NULL: the chosen scores (-inf
+ *             where assign is -1)
+ *   perm, slots, offsets [device] int32 out, as above
+ *   workspace [device] base_topk_workspace_size(T, E, k) bytes, 256-aligned; any
+ *             contents at entry. Calls that overlap in time need their own.
+ * base_sort_by_expert - the same sort for choices that are given (assign [T, k];
+ * an entry outside [0, E) has no expert).
+ * Errors: BASE_ERR_INVALID_ARG, BASE_ERR_RANGE, BASE_ERR_WORKSPACE, BASE_ERR_HIP.
+ */
+size_t base_topk_workspace_size(int64_t T, int64_t E, int64_t k);
+int base_topk_assign(const float *S, int64_t T, int64_t E, int64_t k, int32_t *assign,
+                     float *scores, int32_t *perm, int32_t *slots, int32_t *offsets,
+                     void *workspace, size_t workspace_bytes, void *stream);
+int base_sort_by_expert(const int32_t *assign, int64_t T, int64_t E, int64_t k, int32_t *perm,
+                        int32_t *slots, int32_t *offsets, void *workspace, size_t workspace_bytes,
+                        void *stream);
+
+/*
+ * base_dispatch - token rows to their routed rows:
+ *     out[slots[t, j]] = weights[t, j] in[t]      (weights NULL: a copy, bit for bit)
+ * base_combine - routed rows back to their tokens:
+ *     out[t] = residual[t] + sum over j of weights[t, j] F[slots[t, j]]
+ * (weights NULL: 1, residual NULL: 0; pairs without a row add nothing, whatever
+ * their weight). Without weights each is the gradient of the other.
+ * base_combine_backward - the gradient of base_combine for an upstream dY:
+ *     dF[slots[t, j]] = weights[t, j] dY[t],   dweights[t, j] = dY[t] . F[slots[t, j]]
+ * (dweights 0 for a pair without a row). Sums run in fp32 in the order of j;
+ * bf16 results are rounded once, to nearest even.
+ *   in, residual, out of base_combine, dY  [device] T x d of dtype (BASE_BF16 or
+ *            BASE_F32); out of base_dispatch, F, dF  [device] T k x d
+ *   weights, dweights  [device] float32 [T, k]
+ *   slots    [device] int32 [T, k]; an entry outside [0, T k) is no row (never
+ *            read or written out of bounds). Two pairs with the same row: which
+ *            of them writes it is unspecified.
+ *   d % 8 == 0, d <= 2^20; rows 16-byte aligned. Outputs must not overlap inputs,
+ *   except that out may be residual.
+ * Errors: BASE_ERR_INVALID_ARG, BASE_ERR_UNSUPPORTED_DTYPE, BASE_ERR_RANGE, BASE_ERR_HIP.
+ */
+int base_dispatch(const void *in, const float *weights, const int32_t *slots, void *out, int64_t T,
+                  int64_t k, int64_t d, int dtype, void *stream);
+int base_combine(const void *F, const float *weights, const int32_t *slots, const void *residual,
+                 void *out, int64_t T, int64_t k, int64_t d, int dtype, void *stream);
+int base_combine_backward(const void *dY, const void *F, const float *weights,
+                          const int32_t *slots, void *dF, float *dweights, int64_t T, int64_t k,
+                          int64_t d, int dtype, void *stream);
+
+/*
+ * base_expert_norm - layer norm of N routed rows, each with the weights of its
+ * expert:
+ *     y[r] = (x[s] - mean) rstd weight[e] + bias[e],  s the source of row r:
+ *     s = r (perm NULL; then x_rows = N and k = 1) or s = perm[r] / k, so that with
+ *     the sort vector the tokens' rows are read in place and no routed copy of
+ *     them is needed.
+ * base_expert_norm_backward - its gradient for an upstream dy, all in routed order:
+ *     dx[r] = rstd (h - mean(h) - xh mean(h xh)) + residual[r],  h = weight[e] dy[r],
+ *     dweight[e] = sum dy[r] xh[r],  dbias[e] = sum dy[r]  over expert e's rows
+ * (xh the normalised row). Behind a perm, base_combine without weights adds the
+ * rows of dx to their tokens.
+ *   x        [device] x_rows x d of dtype (BASE_BF16 or BASE_F32)
+ *   weight, bias  [device] E x d of dtype; bias may be NULL
+ *   offsets  [device] int32 [E + 1], or NULL with E = 1: one norm for all rows
+ *   y, dy, dx, residual  [device] N x d of dtype; residual may be NULL. Rows
+ *            outside every range or without a source are left as they are.
+ *   mean, rstd  [device] float32 [N], written by the first, read by the second
+ *   dweight, dbias  [device] float32 [E, d], written entirely (zero for an
+ *            expert without rows); dbias may be NULL
+ *   eps      >= 0, finite
+ *   workspace [device] base_expert_norm_workspace_size(N, E, d) bytes, 256-aligned
+ *   N < 2^31, E <= 2048, d % 8 == 0, d <= 16384; matrices 16-byte aligned. y and dx
+ *   must not overlap x; dx may be dy or residual.
+ * Mean, squares about the mean and all sums are fp32, in a fixed order.
+ * Errors: BASE_ERR_INVALID_ARG, BASE_ERR_UNSUPPORTED_DTYPE, BASE_ERR_RANGE,
+ * BASE_ERR_WORKSPACE, BASE_ERR_HIP.
+ */
+int base_expert_norm(const void *x, const int32_t *perm, int64_t x_rows, int64_t k,
+                     const void *weight, const void *bias, const int32_t *offsets, void *y,
+                     float *mean, float *rstd, int64_t N, int64_t E, int64_t d, double eps,
+                     int dtype, void *stream);
+size_t base_expert_norm_workspace_size(int64_t N, int64_t E, int64_t d);
+int base_expert_norm_backward(const void *dy, const void *x, const int32_t *perm, int64_t x_rows,
+                              int64_t k, const void *weight, const float *mean, const float *rstd,
+                              const int32_t *offsets, const void *residual, void *dx,
+                              float *dweight, float *dbias, int64_t N, int64_t E, int64_t d,
+                              int dtype, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * base_expert_linear - routed rows times their experts' matrices:
+ *     y[r] = act(x[r] w[e]^T + bias[e]) + residual[r]
+ * act the ReLU (relu = 1; a NaN stays one) or nothing (relu = 0).
+ * base_expert_linear_dx - the gradient by the rows:
+ *     dx[r] = dy[r] w[e], and 0 where relu_of[r] is given and not > 0 (relu_of: the
+ *     result of the ReLU that made x, so that dx is the gradient before it)
+ * base_expert_linear_dw - the gradient by the matrices:
+ *     dw[e] = sum over expert e's rows of dy[r] x[r]^T,  db[e] = sum of dy[r]
+ *   x, dx, relu_of  [device] N x K of dtype (BASE_BF16 or BASE_F32)
+ *   y, dy, residual [device] N x O of dtype
+ *   w  [device] E x O x K of dtype; bias [device] E x O of dtype, may be NULL
+ *   dw [device] float32 [E, O, K], db [device] float32 [E, O] (may be NULL),
+ *      written entirely (zero for an expert without rows)
+ *   offsets  [device] int32 [E + 1]. Rows of y and dx outside every range are
+ *      left as they are.
+ *   N < 2^31, E <= 2048, K % 8 == 0, O % 8 == 0, K, O <= 2^20; 16-byte aligned. y
+ *   may be residual and dx may be relu_of; outputs overlap no other input.
+ * Products are summed in fp32 (bf16 products are exact there; fp32 ones are not
+ * reduced), in an order that depends on the sizes only: the same call gives the
+ * same bits every time.
+ * Errors: BASE_ERR_INVALID_ARG, BASE_ERR_UNSUPPORTED_DTYPE, BASE_ERR_RANGE, BASE_ERR_HIP.
+ */
+int base_expert_linear(const void *x, const void *w, const void *bias, const void *residual,
+                       const int32_t *offsets, void *y, int64_t N, int64_t E, int64_t K, int64_t O,
+                       int relu, int dtype, void *stream);
+int base_expert_linear_dx(const void *dy, const void *w, const void *relu_of,
+                          const int32_t *offsets, void *dx, int64_t N, int64_t E, int64_t K,
+                          int64_t O, int dtype, void *stream);
+int base_expert_linear_dw(const void *dy, const void *x, const int32_t *offsets, float *dw,
+                          float *db, int64_t N, int64_t E, int64_t K, int64_t O, int dtype,
+                          void *stream);
+
+/* ------------------------------------------------------------------------ */
 /* Measurement support                                                       */
 /* ------------------------------------------------------------------------ */
 /*

@@ -23,7 +23,9 @@ What it computes, each function citing the passage it follows:
   route_shuffled    shuffle to workers, per-worker solve and route   (Sec. 3.2.1)
   unroute_shuffled  expert rows back to the original token order     (Sec. 3.2.1, Sec. 3)
   gate_combine_shuffled  Eq. 1 over shuffled workers, token order    (Sec. 3.1, 3.2.1)
+  experts           k experts a token, the experts' norm and products, gradients
 """
+from . import experts
 from .affinity import affinity
 from .assign import (
     balanced_counts_ok,
@@ -43,6 +45,7 @@ from .shuffle import gate_combine_shuffled, route_shuffled, unroute_shuffled
 
 __all__ = [
     "affinity",
+    "experts",
     "expert_offsets",
     "gate_backward",
     "gate_combine",

@@ -48,7 +48,10 @@ EXPORTED = ("base_status_string", "base_affinity", "base_affinity_gather",
             "base_assign_batched", "base_assign_status", "base_assign_noalloc", "base_permute", "base_permute_batched",
             "base_greedy_workspace_size", "base_greedy_assign", "base_gate_combine",
             "base_gate_combine_batched", "base_gate_backward", "base_timing_enable",
-            "base_timing_read")
+            "base_timing_read", "base_topk_workspace_size", "base_topk_assign",
+            "base_sort_by_expert", "base_dispatch", "base_combine", "base_combine_backward",
+            "base_expert_norm", "base_expert_norm_workspace_size", "base_expert_norm_backward",
+            "base_expert_linear", "base_expert_linear_dx", "base_expert_linear_dw")
 
 
 class AssignOpts(ctypes.Structure):
@@ -122,6 +125,25 @@ def lib() -> ctypes.CDLL:
         L.base_gate_backward.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, i64,
                                          i64, i32, vp]
         L.base_gate_backward.restype = i32
+        sz = ctypes.c_size_t
+        for name, args in {
+                "topk_assign": [vp, i64, i64, i64, vp, vp, vp, vp, vp, vp, sz, vp],
+                "sort_by_expert": [vp, i64, i64, i64, vp, vp, vp, vp, sz, vp],
+                "dispatch": [vp, vp, vp, vp, i64, i64, i64, i32, vp],
+                "combine": [vp, vp, vp, vp, vp, i64, i64, i64, i32, vp],
+                "combine_backward": [vp, vp, vp, vp, vp, vp, i64, i64, i64, i32, vp],
+                "expert_norm": [vp, vp, i64, i64, vp, vp, vp, vp, vp, vp, i64, i64, i64,
+                                ctypes.c_double, i32, vp],
+                "expert_norm_backward": [vp, vp, vp, i64, i64, vp, vp, vp, vp, vp, vp, vp, vp,
+                                         i64, i64, i64, i32, vp, sz, vp],
+                "expert_linear": [vp, vp, vp, vp, vp, vp, i64, i64, i64, i64, i32, i32, vp],
+                "expert_linear_dx": [vp, vp, vp, vp, vp, i64, i64, i64, i64, i32, vp],
+                "expert_linear_dw": [vp, vp, vp, vp, vp, i64, i64, i64, i64, i32, vp]}.items():
+            fn = getattr(L, "base_" + name)
+            fn.argtypes, fn.restype = args, i32
+        for name in ("topk_workspace_size", "expert_norm_workspace_size"):
+            fn = getattr(L, "base_" + name)
+            fn.argtypes, fn.restype = [i64, i64, i64], sz
         L.base_timing_enable.argtypes = [ctypes.c_int32]
         L.base_timing_enable.restype = i32
         L.base_timing_read.argtypes = [ctypes.POINTER(i64), ctypes.POINTER(ctypes.c_double)]
@@ -485,10 +507,18 @@ def timing_read() -> tuple[int, float]:
     return int(n.value), float(ms.value)
 
 
+from .experts import (Routing, combine, combine_backward, dispatch, expert_linear,  # noqa: E402
+                      expert_linear_dw, expert_linear_dx, expert_norm, expert_norm_backward,
+                      expert_norm_workspace_size, sort_by_expert, topk_assign,
+                      topk_workspace_size)
+
 __all__ = ["affinity", "assign", "assign_batched", "permute", "permute_batched", "greedy_assign",
            "gate_combine", "gate_combine_batched",
            "gate_backward", "balanced_offsets", "assign_workspace_size",
            "assign_batched_workspace_size", "timing_enable",
            "timing_read", "AssignResult", "AssignOpts", "AssignStats", "BaseError", "lib",
            "assign_status", "assign_noalloc", "NOALLOC_MAX_WORKSPACE",
-           "status_string", "EXPORTED"]
+           "status_string", "EXPORTED", "Routing", "topk_assign", "topk_workspace_size",
+           "sort_by_expert", "dispatch", "combine", "combine_backward", "expert_norm",
+           "expert_norm_workspace_size", "expert_norm_backward", "expert_linear",
+           "expert_linear_dx", "expert_linear_dw"]

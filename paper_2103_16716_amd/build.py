@@ -1,6 +1,6 @@
 """Build the HIP library of the assignment path for gfx950.
 
-Compiles csrc/*.hip and csrc/abi.cpp with hipcc into
+Compiles csrc/*.hip and csrc/abi*.cpp with hipcc into
 paper_2103_16716_amd/libbase_mi355x.so (in-tree). Run as
 `python -m paper_2103_16716_amd.build`.
 """
@@ -19,8 +19,8 @@ BUILD_DIR = os.path.join(HERE, "_build")
 ARCH = "gfx950"
 
 SOURCES = ["affinity.hip", "auction.hip", "permute.hip", "gate.hip", "noalloc.hip",
-           "abi.cpp"]
-HEADERS = ["common.hpp", "internal.hpp"]
+           "topk.hip", "moves.hip", "norm.hip", "linear.hip", "abi.cpp", "abi_experts.cpp"]
+HEADERS = ["common.hpp", "internal.hpp", "rows.hpp"]
 
 # Packed fp32 instructions are kept out of the device code on purpose; the
 # host pass warns that it does not know the feature, which is harmless.

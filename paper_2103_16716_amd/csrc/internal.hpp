@@ -107,6 +107,47 @@ hipError_t launch_gate_backward(const void *dY, const void *F, const void *H, co
                                 const int32_t *offsets, void *dH, void *dF, float *dW, float *dS,
                                 int64_t T, int64_t E, int64_t d, int bf16, hipStream_t s);
 
+// The k best experts of each token and the sort of the T k pairs by expert
+// (topk.hip). S null: the choices in assign are given.
+size_t topk_workspace_size(int64_t T, int64_t E, int64_t k);
+hipError_t launch_topk(const float *S, int64_t T, int64_t E, int64_t k, int32_t *assign,
+                       float *scores, int32_t *perm, int32_t *slots, int32_t *offsets,
+                       void *workspace, hipStream_t s);
+
+// Rows of T tokens to their T k routed rows and back (moves.hip).
+hipError_t launch_dispatch(const void *x, const float *w, const int32_t *slots, void *out,
+                           int64_t T, int64_t k, int64_t d, int bf16, hipStream_t s);
+hipError_t launch_combine(const void *F, const float *w, const int32_t *slots,
+                          const void *residual, void *out, int64_t T, int64_t k, int64_t d,
+                          int bf16, hipStream_t s);
+hipError_t launch_combine_backward(const void *dY, const void *F, const float *w,
+                                   const int32_t *slots, void *dF, float *dw, int64_t T, int64_t k,
+                                   int64_t d, int bf16, hipStream_t s);
+
+// Layer norm of N routed rows with their experts' weights (norm.hip). perm null:
+// row r of x; offsets null: one expert.
+size_t norm_workspace_size(int64_t N, int64_t E, int64_t d);
+hipError_t launch_norm(const void *x, const int32_t *perm, int64_t x_rows, int64_t k,
+                       const void *weight, const void *bias, const int32_t *offsets, void *y,
+                       float *mean, float *rstd, int64_t N, int64_t E, int64_t d, double eps,
+                       int bf16, hipStream_t s);
+hipError_t launch_norm_backward(const void *dy, const void *x, const int32_t *perm, int64_t x_rows,
+                                int64_t k, const void *weight, const float *mean,
+                                const float *rstd, const int32_t *offsets, const void *residual,
+                                void *dx, float *dweight, float *dbias, int64_t N, int64_t E,
+                                int64_t d, int bf16, void *workspace, hipStream_t s);
+
+// The experts' products over N routed rows, w [E, O, K] (linear.hip).
+hipError_t launch_linear(const void *x, const void *w, const void *bias, const void *residual,
+                         const int32_t *offsets, void *y, int64_t N, int64_t E, int64_t K,
+                         int64_t O, int relu, int bf16, hipStream_t s);
+hipError_t launch_linear_dx(const void *dy, const void *w, const void *relu_of,
+                            const int32_t *offsets, void *dx, int64_t N, int64_t E, int64_t K,
+                            int64_t O, int bf16, hipStream_t s);
+hipError_t launch_linear_dw(const void *dy, const void *x, const int32_t *offsets, float *dw,
+                            float *db, int64_t N, int64_t E, int64_t K, int64_t O, int bf16,
+                            hipStream_t s);
+
 // Event timing of the engine kernel's launches (measurement support).
 hipError_t timing_enable(int32_t capacity);
 hipError_t timing_read(int64_t *launches, double *total_ms);

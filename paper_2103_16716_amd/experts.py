@@ -1,0 +1,375 @@
+"""k experts a token and the experts themselves: routing, row moves, layer norm
+and products on routed rows, with their gradients.
+
+    r = topk_assign(S, 2)                       # 2 experts a token, rows by expert
+    y, mean, rstd = expert_norm(H, g, b, r.offsets, perm=r.perm, k=2)
+    u = expert_linear(y, W1, r.offsets, bias=b1, relu=True)
+    f = expert_linear(u, W2, r.offsets, bias=b2)
+    out = combine(f, r.slots, weights=torch.softmax(r.scores, 1), residual=H)
+
+and back, for an upstream dOut:
+
+    df, dweights = combine_backward(dOut, f, r.slots, weights)
+    dW2, db2 = expert_linear_dw(df, u, r.offsets)
+    du = expert_linear_dx(df, W2, r.offsets, relu_of=u)
+    dW1, db1 = expert_linear_dw(du, y, r.offsets)
+    dy = expert_linear_dx(du, W1, r.offsets)
+    dx, dg, db = expert_norm_backward(dy, H, g, mean, rstd, r.offsets, perm=r.perm, k=2)
+    dH = combine(dx, r.slots, residual=dOut)
+
+Marshals torch tensors into the C calls of include/base.h. Tensors are contiguous
+and on the current device. Work goes to the current stream, or to `stream`, in
+whose memory pool outputs that are not given are then allocated. Rows that no pair
+has (behind offsets[-1]) are left as they are in outputs that are given, and are
+unspecified in ones that are not.
+"""
+from __future__ import annotations
+
+import contextlib
+import dataclasses
+
+from . import _check, _dtype_code, _stream_ptr, _torch, lib
+
+
+@dataclasses.dataclass
+class Routing:
+    assign: object      # int32 [T, k], -1: no expert
+    scores: object      # float32 [T, k] (None from sort_by_expert)
+    perm: object        # int32 [T k]: pair t k + j of each routed row
+    slots: object       # int32 [T, k]: routed row of each pair, -1: none
+    offsets: object     # int32 [E + 1]: expert e's rows are [offsets[e], offsets[e + 1])
+
+
+def _need(**tensors) -> None:
+    """Every given tensor contiguous and on the current device."""
+    here = None
+    for name, t in tensors.items():
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError(f"{name} must be on the GPU")
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+        if here is None:
+            here = _torch().cuda.current_device()
+        if t.device.index != here:
+            raise ValueError(f"{name} is on {t.device}, the current device is cuda:{here}")
+
+
+def _like(name, t, shape, dtype) -> None:
+    if t is not None and (tuple(t.shape) != tuple(shape) or t.dtype != dtype):
+        raise ValueError(f"{name} must be {dtype} {list(shape)}, not {t.dtype} {list(t.shape)}")
+
+
+def _dims(name, t, n) -> None:
+    if t.dim() != n:
+        raise ValueError(f"{name} must have {n} dimensions")
+
+
+def _on(stream):
+    """Where outputs are allocated: the pool of the stream that writes them."""
+    return contextlib.nullcontext() if stream is None else _torch().cuda.stream(stream)
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _workspace(given, nbytes, device):
+    torch = _torch()
+    if given is not None:
+        _need(workspace=given)
+        return given
+    return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+
+
+def topk_workspace_size(T: int, E: int, k: int) -> int:
+    return int(lib().base_topk_workspace_size(T, E, k))
+
+
+def _routing(T, E, k, dev, out_perm, out_slots, out_offsets):
+    torch = _torch()
+    _need(out_perm=out_perm, out_slots=out_slots, out_offsets=out_offsets)
+    i32 = dict(dtype=torch.int32, device=dev)
+    _like("out_perm", out_perm, (T * k,), torch.int32)
+    _like("out_slots", out_slots, (T, k), torch.int32)
+    _like("out_offsets", out_offsets, (E + 1,), torch.int32)
+    return (torch.empty(T * k, **i32) if out_perm is None else out_perm,
+            torch.empty((T, k), **i32) if out_slots is None else out_slots,
+            torch.empty(E + 1, **i32) if out_offsets is None else out_offsets)
+
+
+def topk_assign(S, k: int, workspace=None, stream=None, out_assign=None, out_scores=None,
+                out_perm=None, out_slots=None, out_offsets=None) -> Routing:
+    """The k best experts of each row of S (float32 [T, E]), highest first, lowest
+    index on ties, never one of score -inf or NaN; and the sort of the pairs by
+    expert (base_topk_assign)."""
+    torch = _torch()
+    _need(S=S, out_assign=out_assign, out_scores=out_scores)
+    _dims("S", S, 2)
+    if S.dtype != torch.float32:
+        raise TypeError("S must be float32")
+    T, E = S.shape
+    k = int(k)
+    if not 0 < k <= min(E, 64):
+        raise ValueError(f"k must be in 1 .. {min(E, 64)}")
+    with _on(stream):
+        _like("out_assign", out_assign, (T, k), torch.int32)
+        _like("out_scores", out_scores, (T, k), torch.float32)
+        assign = out_assign
+        if assign is None:
+            assign = torch.empty((T, k), dtype=torch.int32, device=S.device)
+        scores = out_scores
+        if scores is None:
+            scores = torch.empty((T, k), dtype=torch.float32, device=S.device)
+        perm, slots, offsets = _routing(T, E, k, S.device, out_perm, out_slots, out_offsets)
+        ws = _workspace(workspace, topk_workspace_size(T, E, k), S.device)
+        _check(lib().base_topk_assign(S.data_ptr(), T, E, k, assign.data_ptr(), scores.data_ptr(),
+                                      perm.data_ptr(), slots.data_ptr(), offsets.data_ptr(),
+                                      ws.data_ptr(), ws.numel() * ws.element_size(),
+                                      _stream_ptr(stream)), "base_topk_assign")
+    return Routing(assign, scores, perm, slots, offsets)
+
+
+def sort_by_expert(assign, E: int, workspace=None, stream=None, out_perm=None, out_slots=None,
+                   out_offsets=None) -> Routing:
+    """The sort of topk_assign for given choices, int32 [T, k] (or [T]: one
+    choice); entries outside [0, E) have no expert (base_sort_by_expert)."""
+    torch = _torch()
+    _need(assign=assign)
+    if assign.dtype != torch.int32:
+        raise TypeError("assign must be int32")
+    if assign.dim() == 1:
+        assign = assign.unsqueeze(1)
+    _dims("assign", assign, 2)
+    T, k = assign.shape
+    E = int(E)
+    with _on(stream):
+        perm, slots, offsets = _routing(T, E, k, assign.device, out_perm, out_slots, out_offsets)
+        ws = _workspace(workspace, topk_workspace_size(T, E, k), assign.device)
+        _check(lib().base_sort_by_expert(assign.data_ptr(), T, E, k, perm.data_ptr(),
+                                         slots.data_ptr(), offsets.data_ptr(), ws.data_ptr(),
+                                         ws.numel() * ws.element_size(), _stream_ptr(stream)),
+               "base_sort_by_expert")
+    return Routing(assign, None, perm, slots, offsets)
+
+
+def _slots_of(slots, weights):
+    torch = _torch()
+    _need(slots=slots, weights=weights)
+    _dims("slots", slots, 2)
+    if slots.dtype != torch.int32:
+        raise TypeError("slots must be int32")
+    _like("weights", weights, slots.shape, torch.float32)
+    return slots.shape
+
+
+def dispatch(x, slots, weights=None, out=None, stream=None):
+    """Token rows to their routed rows, out[slots[t, j]] = weights[t, j] x[t]
+    (base_dispatch); out has T k rows. Without weights a copy bit for bit, the
+    gradient of combine without weights."""
+    torch = _torch()
+    T, k = _slots_of(slots, weights)
+    _need(x=x, out=out)
+    _dims("x", x, 2)
+    d = x.shape[1]
+    _like("x", x, (T, d), x.dtype)
+    _like("out", out, (T * k, d), x.dtype)
+    with _on(stream):
+        if out is None:
+            out = torch.empty((T * k, d), dtype=x.dtype, device=x.device)
+        _check(lib().base_dispatch(x.data_ptr(), _ptr(weights), slots.data_ptr(), out.data_ptr(),
+                                   T, k, d, _dtype_code(x), _stream_ptr(stream)), "base_dispatch")
+    return out
+
+
+def combine(F, slots, weights=None, residual=None, out=None, stream=None):
+    """Routed rows back to their tokens, out[t] = residual[t] + sum over j of
+    weights[t, j] F[slots[t, j]] (base_combine). Pairs without a row add nothing."""
+    torch = _torch()
+    T, k = _slots_of(slots, weights)
+    _need(F=F, residual=residual, out=out)
+    _dims("F", F, 2)
+    d = F.shape[1]
+    _like("F", F, (T * k, d), F.dtype)
+    _like("residual", residual, (T, d), F.dtype)
+    _like("out", out, (T, d), F.dtype)
+    with _on(stream):
+        if out is None:
+            out = torch.empty((T, d), dtype=F.dtype, device=F.device)
+        _check(lib().base_combine(F.data_ptr(), _ptr(weights), slots.data_ptr(), _ptr(residual),
+                                  out.data_ptr(), T, k, d, _dtype_code(F), _stream_ptr(stream)),
+               "base_combine")
+    return out
+
+
+def combine_backward(dY, F, slots, weights, out=None, stream=None):
+    """Gradient of combine with weights (base_combine_backward): (dF in routed
+    order, dweights [T, k]). The residual's gradient is dY."""
+    torch = _torch()
+    T, k = _slots_of(slots, weights)
+    _need(dY=dY, F=F, out=out)
+    _dims("F", F, 2)
+    d = F.shape[1]
+    _like("F", F, (T * k, d), F.dtype)
+    _like("dY", dY, (T, d), F.dtype)
+    _like("out", out, (T * k, d), F.dtype)
+    if weights is None:
+        raise ValueError("weights are needed (without them the gradient is dispatch(dY, slots))")
+    with _on(stream):
+        if out is None:
+            out = torch.empty_like(F)
+        dw = torch.empty((T, k), dtype=torch.float32, device=F.device)
+        _check(lib().base_combine_backward(dY.data_ptr(), F.data_ptr(), weights.data_ptr(),
+                                           slots.data_ptr(), out.data_ptr(), dw.data_ptr(), T, k,
+                                           d, _dtype_code(F), _stream_ptr(stream)),
+               "base_combine_backward")
+    return out, dw
+
+
+def _norm_args(x, weight, offsets, perm, k):
+    """(N, E, d, weight as [E, d]) of a norm's arguments."""
+    torch = _torch()
+    _need(x=x, weight=weight, offsets=offsets, perm=perm)
+    _dims("x", x, 2)
+    d = x.shape[1]
+    if weight.dim() == 1:
+        weight = weight.unsqueeze(0)
+    E = weight.shape[0]
+    _like("weight", weight, (E, d), x.dtype)
+    _like("offsets", offsets, (E + 1,), torch.int32)
+    if offsets is None and E != 1:
+        raise ValueError("weights of several experts need offsets")
+    if perm is None and k != 1:
+        raise ValueError("k needs perm")
+    if perm is not None:
+        _dims("perm", perm, 1)
+        _like("perm", perm, perm.shape, torch.int32)
+    return (x.shape[0] if perm is None else perm.shape[0]), E, d
+
+
+def expert_norm(x, weight, bias=None, offsets=None, eps: float = 1e-5, perm=None, k: int = 1,
+                out=None, stream=None):
+    """Layer norm of routed rows with their experts' weights [E, d] (base_expert_norm):
+    (y, mean, rstd). With perm, routed row r is row perm[r] // k of x. Without
+    offsets one norm, weight [d] or [1, d], for every row."""
+    torch = _torch()
+    N, E, d = _norm_args(x, weight, offsets, perm, k)
+    _need(bias=bias, out=out)
+    if bias is not None:
+        _like("bias", bias, weight.shape, x.dtype)
+    _like("out", out, (N, d), x.dtype)
+    with _on(stream):
+        if out is None:
+            out = torch.empty((N, d), dtype=x.dtype, device=x.device)
+        stat = torch.empty((2, N), dtype=torch.float32, device=x.device)
+        mean, rstd = stat[0], stat[1]
+        _check(lib().base_expert_norm(x.data_ptr(), _ptr(perm), x.shape[0], k, weight.data_ptr(),
+                                      _ptr(bias), _ptr(offsets), out.data_ptr(), mean.data_ptr(),
+                                      rstd.data_ptr(), N, E, d, float(eps), _dtype_code(x),
+                                      _stream_ptr(stream)), "base_expert_norm")
+    return out, mean, rstd
+
+
+def expert_norm_workspace_size(N: int, E: int, d: int) -> int:
+    return int(lib().base_expert_norm_workspace_size(N, E, d))
+
+
+def expert_norm_backward(dy, x, weight, mean, rstd, offsets=None, perm=None, k: int = 1,
+                         residual=None, out=None, workspace=None, stream=None):
+    """Gradient of expert_norm (base_expert_norm_backward): (dx, dweight, dbias), dx
+    in routed order with `residual` added, the others float32 of weight's shape."""
+    torch = _torch()
+    N, E, d = _norm_args(x, weight, offsets, perm, k)
+    _need(dy=dy, mean=mean, rstd=rstd, residual=residual, out=out)
+    _like("dy", dy, (N, d), x.dtype)
+    _like("mean", mean, (N,), torch.float32)
+    _like("rstd", rstd, (N,), torch.float32)
+    _like("residual", residual, (N, d), x.dtype)
+    _like("out", out, (N, d), x.dtype)
+    with _on(stream):
+        if out is None:
+            out = torch.empty((N, d), dtype=x.dtype, device=x.device)
+        sums = torch.empty((2, *weight.shape), dtype=torch.float32, device=x.device)
+        dweight, dbias = sums[0], sums[1]
+        ws = _workspace(workspace, expert_norm_workspace_size(N, E, d), x.device)
+        _check(lib().base_expert_norm_backward(
+            dy.data_ptr(), x.data_ptr(), _ptr(perm), x.shape[0], k, weight.data_ptr(),
+            mean.data_ptr(), rstd.data_ptr(), _ptr(offsets), _ptr(residual), out.data_ptr(),
+            dweight.data_ptr(), dbias.data_ptr(), N, E, d, _dtype_code(x), ws.data_ptr(),
+            ws.numel() * ws.element_size(), _stream_ptr(stream)), "base_expert_norm_backward")
+    return out, dweight, dbias
+
+
+def _linear_args(w, offsets):
+    torch = _torch()
+    _need(w=w, offsets=offsets)
+    _dims("w", w, 3)
+    E, O, K = w.shape
+    _like("offsets", offsets, (E + 1,), torch.int32)
+    return E, O, K
+
+
+def expert_linear(x, w, offsets, bias=None, relu: bool = False, residual=None, out=None,
+                  stream=None):
+    """Routed rows x [N, K] times their experts' matrices w [E, O, K]: y = act(x w^T +
+    bias) + residual, act the ReLU with `relu` (base_expert_linear)."""
+    torch = _torch()
+    E, O, K = _linear_args(w, offsets)
+    _need(x=x, bias=bias, residual=residual, out=out)
+    _dims("x", x, 2)
+    N = x.shape[0]
+    _like("x", x, (N, K), w.dtype)
+    _like("bias", bias, (E, O), w.dtype)
+    _like("residual", residual, (N, O), w.dtype)
+    _like("out", out, (N, O), w.dtype)
+    with _on(stream):
+        if out is None:
+            out = torch.empty((N, O), dtype=x.dtype, device=x.device)
+        _check(lib().base_expert_linear(x.data_ptr(), w.data_ptr(), _ptr(bias), _ptr(residual),
+                                        offsets.data_ptr(), out.data_ptr(), N, E, K, O,
+                                        1 if relu else 0, _dtype_code(x), _stream_ptr(stream)),
+               "base_expert_linear")
+    return out
+
+
+def expert_linear_dx(dy, w, offsets, relu_of=None, out=None, stream=None):
+    """Gradient of expert_linear by its rows, dy w (base_expert_linear_dx). With relu_of
+    (the ReLU's result that was x) the gradient before that ReLU: 0 where it is not > 0."""
+    torch = _torch()
+    E, O, K = _linear_args(w, offsets)
+    _need(dy=dy, relu_of=relu_of, out=out)
+    _dims("dy", dy, 2)
+    N = dy.shape[0]
+    _like("dy", dy, (N, O), w.dtype)
+    _like("relu_of", relu_of, (N, K), w.dtype)
+    _like("out", out, (N, K), w.dtype)
+    with _on(stream):
+        if out is None:
+            out = torch.empty((N, K), dtype=dy.dtype, device=dy.device)
+        _check(lib().base_expert_linear_dx(dy.data_ptr(), w.data_ptr(), _ptr(relu_of),
+                                           offsets.data_ptr(), out.data_ptr(), N, E, K, O,
+                                           _dtype_code(dy), _stream_ptr(stream)),
+               "base_expert_linear_dx")
+    return out
+
+
+def expert_linear_dw(dy, x, offsets, stream=None):
+    """Gradient of expert_linear by its matrices and bias (base_expert_linear_dw):
+    (dw float32 [E, O, K], db float32 [E, O]), summed over each expert's rows."""
+    torch = _torch()
+    _need(dy=dy, x=x, offsets=offsets)
+    _dims("dy", dy, 2)
+    _dims("x", x, 2)
+    _dims("offsets", offsets, 1)
+    (N, O), K, E = dy.shape, x.shape[1], offsets.shape[0] - 1
+    _like("x", x, (N, K), dy.dtype)
+    _like("offsets", offsets, (E + 1,), torch.int32)
+    with _on(stream):
+        dw = torch.empty((E, O, K), dtype=torch.float32, device=dy.device)
+        db = torch.empty((E, O), dtype=torch.float32, device=dy.device)
+        _check(lib().base_expert_linear_dw(dy.data_ptr(), x.data_ptr(), offsets.data_ptr(),
+                                           dw.data_ptr(), db.data_ptr(), N, E, K, O,
+                                           _dtype_code(dy), _stream_ptr(stream)),
+               "base_expert_linear_dw")
+    return dw, db

@@ -1,0 +1,141 @@
+"""Refusals of the expert layer's calls, on the host: nothing here reaches the GPU
+(no call carries a full set of valid arguments)."""
+import pytest
+import torch
+
+import paper_2103_16716_amd as pb
+from paper_2103_16716_amd import build as pbuild
+
+FAKE = 0x10000            # 64 KiB-aligned stand-in addresses, never dereferenced
+FAR = FAKE + (1 << 30)
+FURTHER = FAKE + (2 << 30)
+INV, RNG, WS, DT = (pb.BASE_ERR_INVALID_ARG, pb.BASE_ERR_RANGE, pb.BASE_ERR_WORKSPACE,
+                    pb.BASE_ERR_UNSUPPORTED_DTYPE)
+BF16, F32 = pb.BASE_BF16, pb.BASE_F32
+
+
+@pytest.fixture(scope="module")
+def L():
+    if pbuild.is_stale():
+        pbuild.build()
+    return pb.lib()
+
+
+def call(fn, good, **bad):
+    """fn with the arguments of `good`, some replaced."""
+    assert set(bad) <= set(good)
+    return fn(*{**good, **bad}.values())
+
+
+def test_routing(L):
+    g = dict(S=FAKE, T=8, E=4, k=2, assign=FAKE, scores=None, perm=FAKE, slots=FAKE, offsets=FAKE,
+             ws=FAKE, wsb=0, stream=None)
+    f = L.base_topk_assign
+    for name in ("S", "assign", "perm", "slots", "offsets"):
+        assert call(f, g, **{name: None}) == INV
+        assert call(f, g, **{name: FAKE + 2}) == INV
+    for bad in (dict(T=0), dict(E=0), dict(k=0), dict(k=5), dict(T=-1)):
+        assert call(f, g, **bad) == INV
+    for bad in (dict(E=2049), dict(T=1 << 31), dict(T=1 << 30, k=4), dict(E=128, k=65)):
+        assert call(f, g, **bad) == RNG
+    need = pb.topk_workspace_size(8, 4, 2)
+    assert need > 0 and need % 256 == 0
+    assert call(f, g, wsb=need - 1) == WS
+    assert call(f, g, ws=None, wsb=need) == WS
+    assert call(f, g, ws=FAKE + 16, wsb=need) == WS
+    assert pb.topk_workspace_size(0, 4, 2) == 0 and pb.topk_workspace_size(8, 4096, 2) == 0
+    s = dict(assign=FAKE, T=8, E=4, k=5, perm=FAKE, slots=FAKE, offsets=FAKE, ws=FAKE, wsb=0,
+             stream=None)
+    f = L.base_sort_by_expert
+    for name in ("assign", "perm", "slots", "offsets"):
+        assert call(f, s, **{name: None}) == INV
+    assert call(f, s, T=0) == INV and call(f, s, E=4096) == RNG
+    assert call(f, s, wsb=pb.topk_workspace_size(8, 4, 5) - 1) == WS
+
+
+def test_moves(L):
+    g = dict(x=FAKE, w=None, slots=FAKE, out=FAR, T=4, k=2, d=16, dtype=BF16, stream=None)
+    f = L.base_dispatch
+    for bad in (dict(x=None), dict(slots=None), dict(out=None), dict(T=0), dict(k=0), dict(d=12),
+                dict(x=FAKE + 8), dict(out=FAR + 4), dict(slots=FAKE + 1), dict(w=FAKE + 2),
+                dict(out=FAKE + 64)):
+        assert call(f, g, **bad) == INV, bad
+    assert call(f, g, dtype=pb.BASE_I16) == DT
+    assert call(f, g, T=1 << 30, k=2) == RNG and call(f, g, k=65) == RNG
+    g = dict(F=FAKE, w=None, slots=FAKE, residual=None, out=FAR, T=4, k=2, d=16, dtype=F32,
+             stream=None)
+    f = L.base_combine
+    for bad in (dict(F=None), dict(slots=None), dict(out=None), dict(d=4), dict(F=FAKE + 8),
+                dict(residual=FAR + 16), dict(residual=FAR + 8), dict(out=FAKE + 256)):
+        assert call(f, g, **bad) == INV, bad
+    g = dict(dY=FAKE, F=FAR, w=FAKE, slots=FAKE, dF=FURTHER, dw=FURTHER + (1 << 20), T=4, k=2, d=16,
+             dtype=F32, stream=None)
+    f = L.base_combine_backward
+    for bad in (dict(dY=None), dict(F=None), dict(w=None), dict(slots=None), dict(dF=None),
+                dict(dw=None), dict(dF=FAR + 64), dict(dF=FAKE), dict(dw=FAKE), dict(T=-1)):
+        assert call(f, g, **bad) == INV, bad
+
+
+def test_norm(L):
+    g = dict(x=FAKE, perm=None, x_rows=4, k=1, weight=FAKE, bias=None, offsets=None, y=FAR,
+             mean=FAKE, rstd=FAKE, N=4, E=1, d=16, eps=1e-5, dtype=BF16, stream=None)
+    f = L.base_expert_norm
+    for bad in (dict(x=None), dict(weight=None), dict(y=None), dict(mean=None), dict(rstd=None),
+                dict(E=2), dict(k=2), dict(x_rows=3), dict(N=0), dict(d=20), dict(eps=-1.0),
+                dict(eps=float("nan")), dict(eps=float("inf")), dict(y=FAKE + 64),
+                dict(x=FAKE + 8), dict(bias=FAKE + 4), dict(offsets=FAKE + 2),
+                dict(perm=FAKE + 2), dict(perm=FAKE, k=0), dict(perm=FAKE, x_rows=0)):
+        assert call(f, g, **bad) == INV, bad
+    assert call(f, g, dtype=pb.BASE_I16) == DT
+    assert call(f, g, d=16392) == RNG and call(f, g, offsets=FAKE, E=2049) == RNG
+    g = dict(dy=FAKE, x=FAR, perm=None, x_rows=4, k=1, weight=FAKE, mean=FAKE, rstd=FAKE,
+             offsets=None, residual=None, dx=FURTHER, dw=FAKE, db=None, N=4, E=1, d=16, dtype=F32,
+             ws=FAKE, wsb=0, stream=None)
+    f = L.base_expert_norm_backward
+    for bad in (dict(dy=None), dict(x=None), dict(weight=None), dict(mean=None), dict(rstd=None),
+                dict(dx=None), dict(dw=None), dict(dx=FAR + 64), dict(dy=FURTHER + 64),
+                dict(residual=FURTHER + 64), dict(E=3)):
+        assert call(f, g, **bad) == INV, bad
+    need = pb.expert_norm_workspace_size(4, 1, 16)
+    assert need > 0 and call(f, g, wsb=need - 1) == WS and call(f, g, ws=FAKE + 8, wsb=need) == WS
+    assert pb.expert_norm_workspace_size(4, 1, 12) == 0
+
+
+def test_products(L):
+    big = 1 << 28   # apart, each smaller than this
+    at = [FAKE + i * big for i in range(6)]
+    g = dict(x=at[0], w=at[1], bias=None, residual=None, offsets=at[2], y=at[3], N=4, E=2, K=16,
+             O=24, relu=0, dtype=BF16, stream=None)
+    f = L.base_expert_linear
+    for bad in (dict(x=None), dict(w=None), dict(offsets=None), dict(y=None), dict(N=0), dict(E=0),
+                dict(K=12), dict(O=20), dict(relu=2), dict(y=at[0] + 32), dict(y=at[1] + 64),
+                dict(residual=at[3] + 16), dict(x=at[0] + 8), dict(offsets=at[2] + 2)):
+        assert call(f, g, **bad) == INV, bad
+    assert call(f, g, dtype=pb.BASE_I16) == DT
+    assert call(f, g, E=2049) == RNG and call(f, g, K=(1 << 20) + 8) == RNG
+    g = dict(dy=at[0], w=at[1], relu_of=None, offsets=at[2], dx=at[3], N=4, E=2, K=16, O=24,
+             dtype=F32, stream=None)
+    f = L.base_expert_linear_dx
+    for bad in (dict(dy=None), dict(w=None), dict(offsets=None), dict(dx=None), dict(dx=at[0]),
+                dict(relu_of=at[3] + 32), dict(O=4)):
+        assert call(f, g, **bad) == INV, bad
+    g = dict(dy=at[0], x=at[1], offsets=at[2], dw=at[3], db=at[4], N=4, E=2, K=16, O=24, dtype=F32,
+             stream=None)
+    f = L.base_expert_linear_dw
+    for bad in (dict(dy=None), dict(x=None), dict(offsets=None), dict(dw=None), dict(dw=at[1] + 16),
+                dict(db=at[3] + 16), dict(K=-8)):
+        assert call(f, g, **bad) == INV, bad
+
+
+def test_binding_refuses_host_tensors():
+    x = torch.zeros(4, 16)
+    i = torch.zeros(4, 2, dtype=torch.int32)
+    o = torch.zeros(3, dtype=torch.int32)
+    for f in (lambda: pb.topk_assign(x, 2), lambda: pb.sort_by_expert(i, 4),
+              lambda: pb.dispatch(x, i), lambda: pb.combine(x, i),
+              lambda: pb.combine_backward(x, x, i, x), lambda: pb.expert_norm(x, x[0]),
+              lambda: pb.expert_norm_backward(x, x, x[0], x[:, 0], x[:, 0]),
+              lambda: pb.expert_linear(x, x[None], o), lambda: pb.expert_linear_dx(x, x[None], o),
+              lambda: pb.expert_linear_dw(x, x, o)):
+        with pytest.raises(ValueError, match="must be on the GPU"):
+            f()
