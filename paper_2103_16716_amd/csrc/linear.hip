@@ -5,14 +5,30 @@
 //   dx[r] = (dy[r] W_e) where relu_of[r] > 0, else 0
 //   dW_e  = sum over its rows of dy[r] x[r]^T,  db_e = sum of dy[r]
 //
-// Products are summed in fp32. Rows in no expert's range are left alone; an expert
-// without rows has zero dW and db.
+// Products are summed in fp32 on the matrix cores (bf16: v_mfma_f32_32x32x16_bf16; fp32:
+// v_mfma_f32_32x32x2_f32, full fp32 products). Rows in no expert's range are left alone;
+// an expert without rows has zero dW and db.
+//
+// One kernel in three forms, by which index of an operand is contiguous in memory:
+//   kNT  y: x and W both by the contraction (inputs)
+//   kNN  dx: dy by the contraction (outputs), W by the result's columns
+//   kTN  dW: dy and x both across it; the contraction is over the expert's rows
+#include <mutex>
+
 #include "common.hpp"
 #include "internal.hpp"
 #include "rows.hpp"
 
 namespace base {
 namespace {
+
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+
+#define BASE_LDS __attribute__((address_space(3)))
 
 // Tile `tile` of the experts' rows in tiles of BM, expert after expert: its
 // expert, its first row and the end of the expert's rows. Asked by whole waves.
@@ -38,131 +54,444 @@ __device__ inline bool find_row_tile(const int32_t *__restrict__ offsets, int E,
         if (past != 0) {
             const int f = __ffsll((unsigned long long)past) - 1;
             out.e = e0 + f;
-            out.r1 = __shfl(z, f);
-            out.r0 = __shfl(a, f) + (tile - before - __shfl(sum - n, f)) * BM;
+            out.r1 = __builtin_amdgcn_readlane(z, f);
+            out.r0 = __builtin_amdgcn_readlane(a, f) +
+                     (tile - before - __builtin_amdgcn_readlane(sum - n, f)) * BM;
             return true;
         }
-        before += __shfl(sum, 63);
+        before += __builtin_amdgcn_readlane(sum, 63);
     }
     return false;
 }
 
-template <bool BF16>
-__device__ inline float element(const void *p, int64_t i) {
-    if constexpr (BF16) return __uint_as_float((uint32_t)static_cast<const uint16_t *>(p)[i] << 16);
-    else return static_cast<const float *>(p)[i];
-}
-template <bool BF16>
-__device__ inline void put(void *p, int64_t i, float v) {
-    if constexpr (BF16) static_cast<__bf16 *>(p)[i] = (__bf16)v;
-    else static_cast<float *>(p)[i] = v;
-}
 
-// Tiles of 64 x 64 outputs and steps of 16 of the contraction on the vector units.
-// kNT: y; kNN: dx; kTN: dW (and, in the tiles of the first 64 inputs, db).
 enum { kNT, kNN, kTN };
-constexpr int kT = 64, kS = 16;
 
-template <bool BF16, int kForm>
-__global__ __launch_bounds__(256) void linear_kernel(
-    const void *__restrict__ A, const void *__restrict__ B, const void *__restrict__ bias,
-    const void *extra, const int32_t *__restrict__ offsets, void *out, float *__restrict__ db,
-    int N, int E, int K, int O, int relu) {
-    __shared__ float a_lds[kS][kT + 1], b_lds[kS][kT + 1];
-    RowTile rt;
-    const int n0 = blockIdx.x * kT;
-    if constexpr (kForm == kTN) {
-        rt.e = blockIdx.z;
-        rt.r0 = row_bound(offsets, rt.e, N);
-        rt.r1 = row_bound(offsets, rt.e + 1, N);
+// 16 bytes of an operand's contraction per lane. bf16: one instruction multiplies the
+// lanes' 8 elements; fp32: four, instruction i the lanes' element i.
+struct Bf16 {
+    static constexpr bool kBf16 = true;
+    using elem_t = uint16_t;
+    using unit_t = bf16x8_t;
+    static constexpr int kPer = 8;
+    static constexpr int kMma = 1;
+    __device__ static f32x16_t mma(unit_t a, unit_t b, f32x16_t c, int) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+    }
+};
+struct F32 {
+    static constexpr bool kBf16 = false;
+    using elem_t = float;
+    using unit_t = f32x4_t;
+    static constexpr int kPer = 4;
+    static constexpr int kMma = 4;
+    __device__ static f32x16_t mma(unit_t a, unit_t b, f32x16_t c, int i) {
+        return __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], b[i], c, 0, 0, 0);
+    }
+};
+
+// Waits until at most N vector-memory operations of this wave are in flight (loads into
+// LDS count until their data is there) and its LDS reads are done.
+template <int N>
+__device__ inline void wait_first() {
+    static_assert(N >= 0 && N < 64, "vmcnt field");
+    __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4));
+}
+
+// Workgroup barrier with no wait of its own; the empty asm statements keep the compiler
+// from moving memory accesses across it.
+__device__ inline void barrier() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+constexpr int kChunk = 128;            // bytes of the contraction per stage and row
+constexpr int kUnits = kChunk / 16;
+constexpr uint32_t kNowhere = 0x80000000u;   // an offset past every buffer: reads as zero
+
+// A stage of one operand: B rows of the result by one chunk of the contraction, S steps.
+//
+// kAlong (contiguous by the contraction): LDS row r holds result row r, and its 16-byte
+// slot s the row's unit s ^ (r % 8), so that the operand reads, one unit of 32 rows, fall
+// on distinct banks.
+//
+// Across: LDS row s holds step s of the contraction with the B result rows side by side.
+// bf16 operands are read with the transposing LDS load, which gives a lane four steps of
+// its own result row; a load instruction takes four steps of 64 bytes each (and as much
+// 8 steps on), so segments of 64 bytes are exchanged by the step: segment g of step s
+// stands at g ^ (s % 4) (rows of 128 bytes: g ^ (s / 2 % 2)). fp32 operands are read by
+// element; a load takes 128 bytes of steps s and s + 4, so segments of 128 bytes stand at
+// g ^ (s / 4 % 2).
+template <class In, bool kAlong, int B, int kThreads>
+struct Stage {
+    using unit_t = typename In::unit_t;
+    static constexpr int kSize = sizeof(typename In::elem_t);
+    static constexpr int S = kChunk / kSize;              // steps of the contraction
+    static constexpr int kBytes = B * kChunk;
+    static constexpr int kSlots = kBytes / 16 / kThreads; // 16-byte slots per thread
+    static constexpr int kRow = B * kSize;                // bytes of an LDS row (across)
+    static constexpr int kRowUnits = kRow / 16;
+    static_assert(kBytes % (16 * kThreads) == 0, "whole slots");
+    static_assert(kAlong || (kThreads / kRowUnits) % 8 == 0, "a thread's slots swizzle alike");
+
+    __device__ static int exchange(int s) {
+        if constexpr (!In::kBf16) return (s >> 2) & 1;
+        else return B >= 128 ? s & 3 : (s >> 1) & 1;
+    }
+
+    uint32_t at[kSlots];   // offsets of this thread's slots from the chunk's first byte
+    uint32_t unit;         // kAlong: this thread's unit of a row's chunk
+
+    // ld: bytes from a row (across: a step) to the next; across, rows is the number of
+    // result rows left in the matrix (kAlong: those past the end lie behind the buffer).
+    __device__ void init(int64_t ld, int rows) {
+        const int tid = threadIdx.x;
+        if constexpr (kAlong) {
+            unit = (tid % kUnits) ^ ((tid / kUnits) & 7);
+#pragma unroll
+            for (int i = 0; i < kSlots; ++i)
+                at[i] = (uint32_t)((i * kThreads + tid) / kUnits * ld) + unit * 16;
+        } else {
+            const int s0 = tid / kRowUnits;
+            const int u = (tid % kRowUnits) ^ (exchange(s0) << (In::kBf16 ? 2 : 3));
+            const bool in = u * In::kPer < rows;
+#pragma unroll
+            for (int i = 0; i < kSlots; ++i)
+                at[i] = in ? (uint32_t)((i * (kThreads / kRowUnits) + s0) * ld) + u * 16 : kNowhere;
+        }
+    }
+    // base: the chunk's first byte; bytes: up to the end of what may be read; steps: those
+    // of the chunk inside the contraction (kAlong only).
+    __device__ void load(const char *base, uint32_t bytes, int steps, BASE_LDS char *lds) const {
+        const __amdgpu_buffer_rsrc_t rsrc =
+            __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, bytes, 0x00020000);
+        const int wave = threadIdx.x >> 6;
+        const bool in = !kAlong || (int)unit * In::kPer < steps;
+#pragma unroll
+        for (int i = 0; i < kSlots; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                rsrc, (BASE_LDS void *)(lds + (i * kThreads + wave * 64) * 16), 16,
+                (int)(in ? at[i] : kNowhere), 0, 0, 0);
+    }
+    // Unit 2 ks + lane / 32 of the contraction for result row 32 t + lane % 32.
+    __device__ static unit_t read(const char *lds, int t, int ks) {
+        const int lane = threadIdx.x & 63;
+        const int half = lane >> 5;
+        if constexpr (kAlong) {
+            const int r = 32 * t + (lane & 31);
+            return *reinterpret_cast<const unit_t *>(lds + r * kChunk +
+                                                     (((2 * ks + half) ^ (r & 7)) * 16));
+        } else if constexpr (In::kBf16) {
+            const int s = 8 * half + ((lane & 15) >> 2);   // (+ 16 ks + 4 for the second)
+            const int off = s * kRow + ((t ^ exchange(s)) * 4 + ((lane >> 3) & 2) + ((lane >> 1) & 1)) * 16 +
+                            (lane & 1) * 8 + 16 * ks * kRow;
+            const int s2 = s + 4;
+            const int off2 = s2 * kRow + ((t ^ exchange(s2)) * 4 + ((lane >> 3) & 2) + ((lane >> 1) & 1)) * 16 +
+                             (lane & 1) * 8 + 16 * ks * kRow;
+            const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (BASE_LDS s16x4_t *)((BASE_LDS char *)lds + off));
+            const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (BASE_LDS s16x4_t *)((BASE_LDS char *)lds + off2));
+            typedef short s16x8_t __attribute__((ext_vector_type(8)));
+            return __builtin_bit_cast(unit_t, (s16x8_t)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        } else {
+            unit_t v;
+            const int s = 4 * (2 * ks + half);
+            const char *p = lds + s * kRow + (t ^ half) * 128 + (lane & 31) * 4;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const float *>(p + i * kRow);
+            return v;
+        }
+    }
+};
+
+// Blocks go to the eight XCDs in turn. Each XCD takes a run of consecutive tiles, so that
+// its L2 serves tiles that share rows or a matrix.
+__device__ inline int tile_of_block(int tiles) {
+    const int per = (tiles + 7) / 8;
+    const int u = blockIdx.x >> 3;
+    const int t = (blockIdx.x & 7) * per + u;
+    return u < per && t < tiles ? t : -1;
+}
+
+// The experts' row tiles in all.
+__device__ inline int count_row_tiles(const int32_t *__restrict__ offsets, int E, int N, int BM) {
+    int n = 0;
+    for (int e = threadIdx.x & 63; e < E; e += 64) {
+        const int a = row_bound(offsets, e, N), z = row_bound(offsets, e + 1, N);
+        n += z > a ? (z - a + BM - 1) / BM : 0;
+    }
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) n += __shfl_xor(n, off);
+    return __builtin_amdgcn_readfirstlane(n);
+}
+
+template <class In>
+__device__ inline void load4(const void *p, int64_t i, float (&v)[4]) {
+    if constexpr (In::kBf16) {
+        const uint2 x = *reinterpret_cast<const uint2 *>(static_cast<const uint16_t *>(p) + i);
+        v[0] = __uint_as_float(x.x << 16);
+        v[1] = __uint_as_float(x.x & 0xffff0000u);
+        v[2] = __uint_as_float(x.y << 16);
+        v[3] = __uint_as_float(x.y & 0xffff0000u);
     } else {
-        if (!find_row_tile(offsets, E, N, kT, blockIdx.y, rt)) return;
+        const float4 x = *reinterpret_cast<const float4 *>(static_cast<const float *>(p) + i);
+        v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
     }
-    // Output [m0.., n0..] of [m_end, cols]; contraction over [s0, s1).
-    const int m0 = kForm == kTN ? blockIdx.y * kT : rt.r0;
-    const int m_end = kForm == kTN ? O : rt.r1;
-    const int cols = kForm == kNT ? O : K;
-    const int s0 = kForm == kTN ? rt.r0 : 0;
-    const int s1 = kForm == kTN ? rt.r1 : kForm == kNT ? K : O;
-    const int64_t we = (int64_t)rt.e * O * K;
-    const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-    float acc[4][4] = {};
-    float sum[4] = {};
-    for (int s = s0; s < s1; s += kS) {
-        for (int i = threadIdx.x; i < kS * kT; i += 256) {
-            const int q = kForm == kTN ? i / kT : i % kS, m = kForm == kTN ? i % kT : i / kS;
-            const bool in = s + q < s1 && m0 + m < m_end;
-            const int64_t at = kForm == kTN ? (int64_t)(s + q) * O + m0 + m
-                                            : (int64_t)(m0 + m) * (kForm == kNT ? K : O) + s + q;
-            a_lds[q][m] = in ? element<BF16>(A, at) : 0.0f;
-        }
-        for (int i = threadIdx.x; i < kS * kT; i += 256) {
-            const int q = kForm == kNT ? i % kS : i / kT, n = kForm == kNT ? i / kS : i % kT;
-            const bool in = s + q < s1 && n0 + n < cols;
-            const int64_t at = kForm == kTN   ? (int64_t)(s + q) * K + n0 + n
-                               : kForm == kNN ? we + (int64_t)(s + q) * K + n0 + n
-                                              : we + (int64_t)(n0 + n) * K + s + q;
-            b_lds[q][n] = in ? element<BF16>(B, at) : 0.0f;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int q = 0; q < kS; ++q) {
-            float a[4], b[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                a[i] = a_lds[q][ty + 16 * i];
-                b[i] = b_lds[q][tx + 16 * i];
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                sum[i] += a[i];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(a[i], b[j], acc[i][j]);
-            }
-        }
-        __syncthreads();
+}
+template <class In>
+__device__ inline void store4(void *p, int64_t i, const float (&v)[4]) {
+    if constexpr (In::kBf16) {
+        const f32x4_t f = {v[0], v[1], v[2], v[3]};
+        *reinterpret_cast<bf16x4_t *>(static_cast<uint16_t *>(p) + i) =
+            __builtin_convertvector(f, bf16x4_t);
+    } else {
+        *reinterpret_cast<float4 *>(static_cast<float *>(p) + i) = make_float4(v[0], v[1], v[2], v[3]);
     }
+}
+
+struct LinearCall {
+    const void *A, *B, *bias, *extra;   // extra: the residual (kNT) or relu_of (kNN)
+    const int32_t *offsets;
+    void *out;
+    int N, E, K, O, relu;
+};
+
+// BM rows (kTN: outputs) by BN columns of the result per block, WM x WN waves.
+template <class In, int kForm, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN, 1) void linear_kernel(LinearCall c) {
+    using unit_t = typename In::unit_t;
+    using elem_t = typename In::elem_t;
+    constexpr int kThreads = 64 * WM * WN;
+    constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
+    using StageA = Stage<In, kForm != kTN, BM, kThreads>;
+    using StageB = Stage<In, kForm == kNT, BN, kThreads>;
+    constexpr int S = StageA::S;
+    constexpr int64_t kSize = sizeof(elem_t);
+    constexpr int kBytes = StageA::kBytes + StageB::kBytes;
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    const int cols = kForm == kNT ? c.O : c.K;
+    const int nn = (cols + BN - 1) / BN;
+    // The block's tile: rows [m0, m_end), columns from n0, contraction over [s0, s1).
+    int m0, m_end, n0, s0, s1, e;
+    if constexpr (kForm == kTN) {
+        const int nm = (c.O + BM - 1) / BM;
+        const int t = tile_of_block(c.E * nm * nn);
+        if (t < 0) return;
+        e = t / (nm * nn);
+        const int r = t - e * nm * nn;
+        m0 = r / nn * BM;
+        n0 = r % nn * BN;
+        m_end = c.O;
+        s0 = __builtin_amdgcn_readfirstlane(row_bound(c.offsets, e, c.N));
+        s1 = __builtin_amdgcn_readfirstlane(row_bound(c.offsets, e + 1, c.N));
+    } else {
+        const int t = tile_of_block(count_row_tiles(c.offsets, c.E, c.N, BM) * nn);
+        if (t < 0) return;
+        RowTile rt;
+        if (!find_row_tile(c.offsets, c.E, c.N, BM, t / nn, rt)) return;
+        e = rt.e;
+        m0 = rt.r0;
+        m_end = rt.r1;
+        n0 = t % nn * BN;
+        s0 = 0;
+        s1 = kForm == kNT ? c.K : c.O;
+    }
+    const int rows = m_end - m0 < BM ? m_end - m0 : BM;
+    const int64_t lda = (int64_t)(kForm == kNT ? c.K : c.O) * sizeof(elem_t);
+    const int64_t ldb = (int64_t)c.K * sizeof(elem_t);
+    const char *A = static_cast<const char *>(c.A), *B = static_cast<const char *>(c.B);
+    if constexpr (kForm != kTN) B += (int64_t)e * c.O * ldb;
+    // First byte of chunk 0 of either operand.
+    A += kForm == kTN ? s0 * lda + m0 * kSize : m0 * lda;
+    B += kForm == kTN   ? s0 * ldb + n0 * kSize
+         : kForm == kNN ? n0 * kSize
+                        : n0 * ldb;
+    const int ncols = cols - n0 < BN ? cols - n0 : BN;
+    StageA sa;
+    StageB sb;
+    sa.init(lda, rows);
+    sb.init(ldb, ncols);
+    const int nk = (s1 - s0 + S - 1) / S;
+    auto issue = [&](int kc, int st) {
+        BASE_LDS char *base = (BASE_LDS char *)lds + st * kBytes;
+        const int left = s1 - s0 - kc * S;   // steps from this chunk on
+        const int steps = left < S ? left : S;
+        const int64_t step_a = kForm == kTN ? S * lda : kChunk;
+        const int64_t step_b = kForm == kNT ? kChunk : S * ldb;
+        const int64_t end_a = kForm == kTN ? steps * lda - m0 * kSize : rows * lda - kc * kChunk;
+        const int64_t end_b = kForm == kNT ? ncols * ldb - kc * kChunk : steps * ldb - n0 * kSize;
+        sa.load(A + kc * step_a, (uint32_t)end_a, left, base);
+        sb.load(B + kc * step_b, (uint32_t)end_b, left, base + StageA::kBytes);
+    };
+    const int wave = threadIdx.x >> 6;
+    const int wm = wave % WM, wn = wave / WM;
+    f32x16_t acc[TM][TN];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int m = m0 + ty + 16 * i;
+    for (int x = 0; x < TM; ++x)
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[x][j][i] = 0.0f;
+    unit_t a[2][TM], b[2][TN];
+    auto fetch = [&](int set, const char *st, int ks) {
+#pragma unroll
+        for (int x = 0; x < TM; ++x) a[set][x] = StageA::read(st, wm * TM + x, ks);
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+            b[set][j] = StageB::read(st + StageA::kBytes, wn * TN + j, ks);
+    };
+    auto multiply = [&](int set) {
+#pragma unroll
+        for (int i = 0; i < In::kMma; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int x = 0; x < TM; ++x)
+                    acc[x][j] = In::mma(b[set][j], a[set][x], acc[x][j], i);
+    };
+    // Two stages. The last quarter of a chunk is multiplied behind the barrier that hands
+    // its stage over: its operands are in registers by then, and the next chunk's first
+    // ones are read beside it.
+    if (nk > 0) {
+        issue(0, 0);
+        if (nk > 1) issue(1, 1);
+        if (nk > 1) wait_first<StageA::kSlots + StageB::kSlots>();
+        else wait_first<0>();
+        barrier();
+        fetch(0, lds, 0);
+        for (int kc = 0; kc < nk; ++kc) {
+            const char *cur = lds + (kc & 1) * kBytes;
+            const char *next = lds + (~kc & 1) * kBytes;
+            fetch(1, cur, 1);
+            multiply(0);
+            fetch(0, cur, 2);
+            multiply(1);
+            fetch(1, cur, 3);
+            multiply(0);
+            wait_first<0>();
+            barrier();
+            if (kc + 1 < nk) fetch(0, next, 0);
+            if (kc + 2 < nk) issue(kc + 2, kc & 1);
+            multiply(1);
+        }
+    }
+    // 32x32 results: lane holds row lane % 32; register i column 8 (i / 4) + 4 (lane / 32) +
+    // i % 4, so four consecutive columns at a time.
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int x = 0; x < TM; ++x) {
+        const int m = m0 + 32 * (wm * TM + x) + (lane & 31);
         if (m >= m_end) continue;
-        if (kForm == kTN && db != nullptr && n0 == 0 && tx == 0) db[(int64_t)rt.e * O + m] = sum[i];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int n = n0 + tx + 16 * j;
-            if (n >= cols) continue;
-            float v = acc[i][j];
-            const int64_t at = (int64_t)m * cols + n;
-            if constexpr (kForm == kTN) {
-                static_cast<float *>(out)[we + at] = v;
-            } else {
-                if (kForm == kNT) {
-                    if (bias != nullptr) v += element<BF16>(bias, (int64_t)rt.e * O + n);
-                    if (relu) v = v < 0.0f ? 0.0f : v;
-                    if (extra != nullptr) v += element<BF16>(extra, at);
-                } else if (extra != nullptr && !(element<BF16>(extra, at) > 0.0f)) {
-                    v = 0.0f;
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int n = n0 + 32 * (wn * TN + j) + 8 * q + 4 * (lane >> 5);
+                if (n >= cols) continue;
+                float v[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] = acc[x][j][4 * q + i];
+                const int64_t at = (int64_t)m * cols + n;
+                if constexpr (kForm == kTN) {
+                    *reinterpret_cast<float4 *>(static_cast<float *>(c.out) +
+                                                (int64_t)e * c.O * c.K + at) =
+                        make_float4(v[0], v[1], v[2], v[3]);
+                } else {
+                    float u[4];
+                    if (kForm == kNT && c.bias != nullptr) {
+                        load4<In>(c.bias, (int64_t)e * c.O + n, u);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) v[i] += u[i];
+                    }
+                    if (kForm == kNT && c.relu) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) v[i] = v[i] < 0.0f ? 0.0f : v[i];
+                    }
+                    if (c.extra != nullptr) {
+                        load4<In>(c.extra, at, u);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            if (kForm == kNT) v[i] += u[i];
+                            else v[i] = u[i] > 0.0f ? v[i] : 0.0f;
+                        }
+                    }
+                    store4<In>(c.out, at, v);
                 }
-                put<BF16>(out, at, v);
             }
+    }
+}
+
+// db_e: column sums of dy over each expert's rows. A block for 128 bytes of an expert's
+// columns: eight lanes take a row's eight chunks, 32 rows in turn over four waves.
+template <bool BF16>
+__global__ __launch_bounds__(256) void row_sums_kernel(const void *__restrict__ dy,
+                                                       const int32_t *__restrict__ offsets,
+                                                       float *__restrict__ db, int N, int O) {
+    using Ck = RowChunk<BF16>;
+    __shared__ float lds[32][8 * Ck::kN + 1];
+    const int e = blockIdx.y;
+    const int ncs = O / Ck::kN;
+    const int c = blockIdx.x * 8 + threadIdx.x % 8;
+    const int g = threadIdx.x / 8;
+    const int a = row_bound(offsets, e, N), z = row_bound(offsets, e + 1, N);
+    float s[Ck::kN];
+#pragma unroll
+    for (int q = 0; q < Ck::kN; ++q) s[q] = 0.0f;
+    if (c < ncs) {
+#pragma unroll 4
+        for (int r = a + g; r < z; r += 32) {
+            float v[Ck::kN];
+            Ck::widen(Ck::fetch(dy, (int64_t)r * ncs + c), v);
+#pragma unroll
+            for (int q = 0; q < Ck::kN; ++q) s[q] += v[q];
         }
     }
+#pragma unroll
+    for (int q = 0; q < Ck::kN; ++q) lds[g][threadIdx.x % 8 * Ck::kN + q] = s[q];
+    __syncthreads();
+    const int i = threadIdx.x;
+    const int col = blockIdx.x * 8 * Ck::kN + i;
+    if (i < 8 * Ck::kN && col < O) {
+        float sum = 0.0f;
+        for (int r = 0; r < 32; ++r) sum += lds[r][i];
+        db[(int64_t)e * O + col] = sum;
+    }
+}
+
+template <class In, int kForm, int BM, int BN, int WM, int WN>
+hipError_t launch_tiles(const LinearCall &c, hipStream_t s) {
+    constexpr size_t kLds = 2 * (size_t)(BM + BN) * kChunk;
+    const auto kernel = &linear_kernel<In, kForm, BM, BN, WM, WN>;
+    if constexpr (kLds > 65536) {   // opted in once per device
+        static std::mutex m;
+        static bool granted[64] = {};
+        int dev = 0;
+        if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return hipErrorInvalidDevice;
+        std::lock_guard<std::mutex> lock(m);
+        if (!granted[dev]) {
+            const hipError_t err =
+                hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
+                                    hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLds);
+            if (err != hipSuccess) return err;
+            granted[dev] = true;
+        }
+    }
+    const int64_t nn = ((kForm == kNT ? c.O : c.K) + BN - 1) / BN;
+    const int64_t nm = kForm == kTN ? (int64_t)c.E * ((c.O + BM - 1) / BM)
+                                    : (int64_t)c.N / BM + (c.E < c.N ? c.E : c.N);
+    const int64_t blocks = (nm * nn + 7) / 8 * 8;
+    if (blocks * 64 * WM * WN >= (int64_t)1 << 32) return hipErrorInvalidConfiguration;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(64 * WM * WN), kLds, s, c);
+    return hipGetLastError();
 }
 
 template <int kForm>
-hipError_t launch_as(const void *A, const void *B, const void *bias, const void *extra,
-                     const int32_t *offsets, void *out, float *db, int64_t N, int64_t E, int64_t K,
-                     int64_t O, int relu, int bf16, hipStream_t s) {
-    const int64_t cols = kForm == kNT ? O : K;
-    const int64_t rows = kForm == kTN ? (O + kT - 1) / kT : N / kT + (E < N ? E : N);
-    const dim3 grid((unsigned)((cols + kT - 1) / kT), (unsigned)rows, kForm == kTN ? (unsigned)E : 1);
-    if (bf16)
-        hipLaunchKernelGGL((linear_kernel<true, kForm>), grid, dim3(256), 0, s, A, B, bias, extra,
-                           offsets, out, db, (int)N, (int)E, (int)K, (int)O, relu);
-    else
-        hipLaunchKernelGGL((linear_kernel<false, kForm>), grid, dim3(256), 0, s, A, B, bias, extra,
-                           offsets, out, db, (int)N, (int)E, (int)K, (int)O, relu);
-    return hipGetLastError();
+hipError_t launch_form(const LinearCall &c, int bf16, hipStream_t s) {
+    if (!bf16) return launch_tiles<F32, kForm, 128, 128, 2, 2>(c, s);
+    if (kForm == kTN || c.N >= 128 * c.E) return launch_tiles<Bf16, kForm, 256, 256, 4, 2>(c, s);
+    return launch_tiles<Bf16, kForm, 64, 128, 2, 2>(c, s);
 }
 
 }  // namespace
@@ -170,19 +499,31 @@ hipError_t launch_as(const void *A, const void *B, const void *bias, const void 
 hipError_t launch_linear(const void *x, const void *w, const void *bias, const void *residual,
                          const int32_t *offsets, void *y, int64_t N, int64_t E, int64_t K,
                          int64_t O, int relu, int bf16, hipStream_t s) {
-    return launch_as<kNT>(x, w, bias, residual, offsets, y, nullptr, N, E, K, O, relu, bf16, s);
+    return launch_form<kNT>({x, w, bias, residual, offsets, y, (int)N, (int)E, (int)K, (int)O, relu},
+                            bf16, s);
 }
 
 hipError_t launch_linear_dx(const void *dy, const void *w, const void *relu_of,
                             const int32_t *offsets, void *dx, int64_t N, int64_t E, int64_t K,
                             int64_t O, int bf16, hipStream_t s) {
-    return launch_as<kNN>(dy, w, nullptr, relu_of, offsets, dx, nullptr, N, E, K, O, 0, bf16, s);
+    return launch_form<kNN>({dy, w, nullptr, relu_of, offsets, dx, (int)N, (int)E, (int)K, (int)O, 0},
+                            bf16, s);
 }
 
 hipError_t launch_linear_dw(const void *dy, const void *x, const int32_t *offsets, float *dw,
                             float *db, int64_t N, int64_t E, int64_t K, int64_t O, int bf16,
                             hipStream_t s) {
-    return launch_as<kTN>(dy, x, nullptr, nullptr, offsets, dw, db, N, E, K, O, 0, bf16, s);
+    const hipError_t err = launch_form<kTN>(
+        {dy, x, nullptr, nullptr, offsets, dw, (int)N, (int)E, (int)K, (int)O, 0}, bf16, s);
+    if (err != hipSuccess || db == nullptr) return err;
+    const dim3 grid((unsigned)((O * (bf16 ? 2 : 4) + 127) / 128), (unsigned)E);
+    if (bf16)
+        hipLaunchKernelGGL(row_sums_kernel<true>, grid, dim3(256), 0, s, dy, offsets, db, (int)N,
+                           (int)O);
+    else
+        hipLaunchKernelGGL(row_sums_kernel<false>, grid, dim3(256), 0, s, dy, offsets, db, (int)N,
+                           (int)O);
+    return hipGetLastError();
 }
 
 }  // namespace base
