@@ -113,8 +113,8 @@ constexpr uint32_t kNowhere = 0x80000000u;   // an offset past every buffer: rea
 // A stage of one operand: B rows of the result by one chunk of the contraction, S steps.
 //
 // kAlong (contiguous by the contraction): LDS row r holds result row r, and its 16-byte
-// slot s the row's unit s ^ (r % 8), so that the operand reads, one unit of 32 rows, fall
-// on distinct banks.
+// slot s the row's unit s ^ (r / 2 % 8): the operand reads take one unit of 16 rows a
+// cycle, and two rows fill the banks.
 //
 // Across: LDS row s holds step s of the contraction with the B result rows side by side.
 // bf16 operands are read with the transposing LDS load, which gives a lane four steps of
@@ -148,7 +148,7 @@ struct Stage {
     __device__ void init(int64_t ld, int rows) {
         const int tid = threadIdx.x;
         if constexpr (kAlong) {
-            unit = (tid % kUnits) ^ ((tid / kUnits) & 7);
+            unit = (tid % kUnits) ^ ((tid / kUnits >> 1) & 7);
 #pragma unroll
             for (int i = 0; i < kSlots; ++i)
                 at[i] = (uint32_t)((i * kThreads + tid) / kUnits * ld) + unit * 16;
@@ -181,7 +181,7 @@ struct Stage {
         if constexpr (kAlong) {
             const int r = 32 * t + (lane & 31);
             return *reinterpret_cast<const unit_t *>(lds + r * kChunk +
-                                                     (((2 * ks + half) ^ (r & 7)) * 16));
+                                                     (((2 * ks + half) ^ ((r >> 1) & 7)) * 16));
         } else if constexpr (In::kBf16) {
             const int s = 8 * half + ((lane & 15) >> 2);   // (+ 16 ks + 4 for the second)
             const int off = s * kRow + ((t ^ exchange(s)) * 4 + ((lane >> 3) & 2) + ((lane >> 1) & 1)) * 16 +
