@@ -108,6 +108,7 @@ __device__ inline void barrier() {
 
 constexpr int kChunk = 128;            // bytes of the contraction per stage and row
 constexpr int kUnits = kChunk / 16;
+constexpr int64_t kUnitsOfDevice = 256;
 constexpr uint32_t kNowhere = 0x80000000u;   // an offset past every buffer: reads as zero
 
 // A stage of one operand: B rows of the result by one chunk of the contraction, S steps.
@@ -206,15 +207,6 @@ struct Stage {
     }
 };
 
-// Blocks go to the eight XCDs in turn. Each XCD takes a run of consecutive tiles, so that
-// its L2 serves tiles that share rows or a matrix.
-__device__ inline int tile_of_block(int tiles) {
-    const int per = (tiles + 7) / 8;
-    const int u = blockIdx.x >> 3;
-    const int t = (blockIdx.x & 7) * per + u;
-    return u < per && t < tiles ? t : -1;
-}
-
 // The experts' row tiles in all.
 __device__ inline int count_row_tiles(const int32_t *__restrict__ offsets, int E, int N, int BM) {
     int n = 0;
@@ -227,27 +219,37 @@ __device__ inline int count_row_tiles(const int32_t *__restrict__ offsets, int E
     return __builtin_amdgcn_readfirstlane(n);
 }
 
-template <class In>
-__device__ inline void load4(const void *p, int64_t i, float (&v)[4]) {
-    if constexpr (In::kBf16) {
-        const uint2 x = *reinterpret_cast<const uint2 *>(static_cast<const uint16_t *>(p) + i);
-        v[0] = __uint_as_float(x.x << 16);
-        v[1] = __uint_as_float(x.x & 0xffff0000u);
-        v[2] = __uint_as_float(x.y << 16);
-        v[3] = __uint_as_float(x.y & 0xffff0000u);
-    } else {
-        const float4 x = *reinterpret_cast<const float4 *>(static_cast<const float *>(p) + i);
-        v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
-    }
+// The tile of a call's `tiles` that a block computes as its i-th. Blocks go to the eight
+// XCDs in turn; each XCD takes a run of consecutive tiles, which share rows or a matrix, so
+// that its L2 serves them. -1: none.
+__device__ inline int tile_of_block(int tiles, int i) {
+    const int per = (tiles + 7) / 8;
+    const int u = (blockIdx.x >> 3) + i * (gridDim.x >> 3);
+    const int t = (blockIdx.x & 7) * per + u;
+    return u < per && t < tiles ? t : -1;
 }
+
+// Tile i of an expert's nm x nn, in strips of kStrip tiles of rows: neighbours in a strip
+// share columns, and the strip's rows stay in the L2 while its columns go by.
+constexpr int kStrip = 4;
+__device__ inline void tile_in_strip(int i, int nm, int nn, int &m, int &n) {
+    const int s = i / (kStrip * nn);
+    const int r = i - s * kStrip * nn;
+    const int h = nm - s * kStrip < kStrip ? nm - s * kStrip : kStrip;
+    n = r / h;
+    m = s * kStrip + r - n * h;
+}
+
 template <class In>
-__device__ inline void store4(void *p, int64_t i, const float (&v)[4]) {
+__device__ inline void load8(const void *p, int64_t i, float (&v)[8]) {
     if constexpr (In::kBf16) {
-        const f32x4_t f = {v[0], v[1], v[2], v[3]};
-        *reinterpret_cast<bf16x4_t *>(static_cast<uint16_t *>(p) + i) =
-            __builtin_convertvector(f, bf16x4_t);
+        const u32x4_t x = *reinterpret_cast<const u32x4_t *>(static_cast<const uint16_t *>(p) + i);
+        RowChunk<true>::widen(x, v);
     } else {
-        *reinterpret_cast<float4 *>(static_cast<float *>(p) + i) = make_float4(v[0], v[1], v[2], v[3]);
+        const float4 *q = reinterpret_cast<const float4 *>(static_cast<const float *>(p) + i);
+        const float4 x = q[0], y = q[1];
+        v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
+        v[4] = y.x, v[5] = y.y, v[6] = y.z, v[7] = y.w;
     }
 }
 
@@ -258,109 +260,109 @@ struct LinearCall {
     int N, E, K, O, relu;
 };
 
-// BM rows (kTN: outputs) by BN columns of the result per block, WM x WN waves.
+// A tile of the result: expert, rows [m0, m_end), columns from n0, contraction [s0, s1).
+struct Tile {
+    int e, m0, m_end, n0, s0, s1;
+};
+
+// BM rows (kTN: outputs) by BN columns of the result, WM x WN waves. A wave has every WM-th
+// 32 rows and TN x 32 neighbouring columns, so that a tile with few rows left (the end of an
+// expert) is spread over the waves, which skip what lies behind: the loop is compiled for
+// each number of 32 rows a wave may have.
 template <class In, int kForm, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN, 1) void linear_kernel(LinearCall c) {
+struct Tiles {
     using unit_t = typename In::unit_t;
     using elem_t = typename In::elem_t;
-    constexpr int kThreads = 64 * WM * WN;
-    constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
+    static constexpr int kThreads = 64 * WM * WN;
+    static constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
     using StageA = Stage<In, kForm != kTN, BM, kThreads>;
     using StageB = Stage<In, kForm == kNT, BN, kThreads>;
-    constexpr int S = StageA::S;
-    constexpr int64_t kSize = sizeof(elem_t);
-    constexpr int kBytes = StageA::kBytes + StageB::kBytes;
-    extern __shared__ __attribute__((aligned(1024))) char lds[];
-    const int cols = kForm == kNT ? c.O : c.K;
-    const int nn = (cols + BN - 1) / BN;
-    // The block's tile: rows [m0, m_end), columns from n0, contraction over [s0, s1).
-    int m0, m_end, n0, s0, s1, e;
-    if constexpr (kForm == kTN) {
-        const int nm = (c.O + BM - 1) / BM;
-        const int t = tile_of_block(c.E * nm * nn);
-        if (t < 0) return;
-        e = t / (nm * nn);
-        const int r = t - e * nm * nn;
-        m0 = r / nn * BM;
-        n0 = r % nn * BN;
-        m_end = c.O;
-        s0 = __builtin_amdgcn_readfirstlane(row_bound(c.offsets, e, c.N));
-        s1 = __builtin_amdgcn_readfirstlane(row_bound(c.offsets, e + 1, c.N));
-    } else {
-        const int t = tile_of_block(count_row_tiles(c.offsets, c.E, c.N, BM) * nn);
-        if (t < 0) return;
-        RowTile rt;
-        if (!find_row_tile(c.offsets, c.E, c.N, BM, t / nn, rt)) return;
-        e = rt.e;
-        m0 = rt.r0;
-        m_end = rt.r1;
-        n0 = t % nn * BN;
-        s0 = 0;
-        s1 = kForm == kNT ? c.K : c.O;
-    }
-    const int rows = m_end - m0 < BM ? m_end - m0 : BM;
-    const int64_t lda = (int64_t)(kForm == kNT ? c.K : c.O) * sizeof(elem_t);
-    const int64_t ldb = (int64_t)c.K * sizeof(elem_t);
-    const char *A = static_cast<const char *>(c.A), *B = static_cast<const char *>(c.B);
-    if constexpr (kForm != kTN) B += (int64_t)e * c.O * ldb;
-    // First byte of chunk 0 of either operand.
-    A += kForm == kTN ? s0 * lda + m0 * kSize : m0 * lda;
-    B += kForm == kTN   ? s0 * ldb + n0 * kSize
-         : kForm == kNN ? n0 * kSize
-                        : n0 * ldb;
-    const int ncols = cols - n0 < BN ? cols - n0 : BN;
+    static constexpr int S = StageA::S;
+    static constexpr int64_t kSize = sizeof(elem_t);
+    static constexpr int kBytes = StageA::kBytes + StageB::kBytes;
+    static constexpr int kLoads = StageA::kSlots + StageB::kSlots;   // of a wave, per stage
+    static constexpr int kOutSize = kForm == kTN ? 4 : (int)kSize;
+
+    const LinearCall &c;
+    char *lds;
     StageA sa;
     StageB sb;
-    sa.init(lda, rows);
-    sb.init(ldb, ncols);
-    const int nk = (s1 - s0 + S - 1) / S;
-    auto issue = [&](int kc, int st) {
-        BASE_LDS char *base = (BASE_LDS char *)lds + st * kBytes;
-        const int left = s1 - s0 - kc * S;   // steps from this chunk on
+    const char *A, *B;
+    int64_t lda, ldb;
+    int cols, wm, wn, lane;
+    Tile t;
+    int nk, ncols;
+
+    __device__ Tiles(const LinearCall &call, char *l) : c(call), lds(l) {
+        cols = kForm == kNT ? c.O : c.K;
+        lda = (kForm == kNT ? c.K : c.O) * kSize;
+        ldb = c.K * kSize;
+        const int wave = threadIdx.x >> 6;
+        lane = threadIdx.x & 63;
+        wm = wave / WN;
+        wn = wave % WN;
+    }
+    // Makes `tile` the one whose chunks are loaded.
+    __device__ void set(const Tile &tile) {
+        t = tile;
+        ncols = cols - t.n0 < BN ? cols - t.n0 : BN;
+        sa.init(lda, t.m_end - t.m0);
+        sb.init(ldb, ncols);
+        A = static_cast<const char *>(c.A);
+        B = static_cast<const char *>(c.B);
+        if (kForm != kTN) B += (int64_t)t.e * c.O * ldb;
+        A += kForm == kTN ? t.s0 * lda + t.m0 * kSize : t.m0 * lda;
+        B += kForm == kTN ? t.s0 * ldb + t.n0 * kSize : kForm == kNN ? t.n0 * kSize : t.n0 * ldb;
+        nk = (t.s1 - t.s0 + S - 1) / S;
+    }
+    __device__ void issue(int kc) const {
+        BASE_LDS char *base = (BASE_LDS char *)lds + (kc & 1) * kBytes;
+        const int left = t.s1 - t.s0 - kc * S;   // steps from this chunk on
         const int steps = left < S ? left : S;
+        const int rows = t.m_end - t.m0 < BM ? t.m_end - t.m0 : BM;
         const int64_t step_a = kForm == kTN ? S * lda : kChunk;
         const int64_t step_b = kForm == kNT ? kChunk : S * ldb;
-        const int64_t end_a = kForm == kTN ? steps * lda - m0 * kSize : rows * lda - kc * kChunk;
-        const int64_t end_b = kForm == kNT ? ncols * ldb - kc * kChunk : steps * ldb - n0 * kSize;
+        const int64_t end_a = kForm == kTN ? steps * lda - t.m0 * kSize : rows * lda - kc * kChunk;
+        const int64_t end_b = kForm == kNT ? ncols * ldb - kc * kChunk : steps * ldb - t.n0 * kSize;
         sa.load(A + kc * step_a, (uint32_t)end_a, left, base);
         sb.load(B + kc * step_b, (uint32_t)end_b, left, base + StageA::kBytes);
-    };
-    const int wave = threadIdx.x >> 6;
-    const int wm = wave % WM, wn = wave / WM;
-    f32x16_t acc[TM][TN];
+    }
+    __device__ void issue_first() const {
+        if (nk > 0) issue(0);
+        if (nk > 1) issue(1);
+    }
+
+    // The products of the tile, whose first chunks have been issued and whose chunk 0 has
+    // landed for this wave. Two stages. The last quarter of a chunk is multiplied behind the
+    // barrier that hands its stage over: its operands are in registers by then, and the
+    // next chunk's first ones are read beside it. Behind the last barrier both stages are free.
+    template <int X>
+    __device__ void contract(f32x16_t (&acc)[X][TN]) const {
 #pragma unroll
-    for (int x = 0; x < TM; ++x)
-#pragma unroll
-        for (int j = 0; j < TN; ++j)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) acc[x][j][i] = 0.0f;
-    unit_t a[2][TM], b[2][TN];
-    auto fetch = [&](int set, const char *st, int ks) {
-#pragma unroll
-        for (int x = 0; x < TM; ++x) a[set][x] = StageA::read(st, wm * TM + x, ks);
-#pragma unroll
-        for (int j = 0; j < TN; ++j)
-            b[set][j] = StageB::read(st + StageA::kBytes, wn * TN + j, ks);
-    };
-    auto multiply = [&](int set) {
-#pragma unroll
-        for (int i = 0; i < In::kMma; ++i)
+        for (int x = 0; x < X; ++x)
 #pragma unroll
             for (int j = 0; j < TN; ++j)
 #pragma unroll
-                for (int x = 0; x < TM; ++x)
-                    acc[x][j] = In::mma(b[set][j], a[set][x], acc[x][j], i);
-    };
-    // Two stages. The last quarter of a chunk is multiplied behind the barrier that hands
-    // its stage over: its operands are in registers by then, and the next chunk's first
-    // ones are read beside it.
-    if (nk > 0) {
-        issue(0, 0);
-        if (nk > 1) issue(1, 1);
-        if (nk > 1) wait_first<StageA::kSlots + StageB::kSlots>();
-        else wait_first<0>();
+                for (int i = 0; i < 16; ++i) acc[x][j][i] = 0.0f;
+        unit_t a[2][X], b[2][TN];
+        auto fetch = [&](int set, const char *st, int ks) {
+#pragma unroll
+            for (int x = 0; x < X; ++x) a[set][x] = StageA::read(st, wm + WM * x, ks);
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+                b[set][j] = StageB::read(st + StageA::kBytes, wn * TN + j, ks);
+        };
+        auto multiply = [&](int set) {
+#pragma unroll
+            for (int i = 0; i < In::kMma; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+#pragma unroll
+                    for (int x = 0; x < X; ++x)
+                        acc[x][j] = In::mma(b[set][j], a[set][x], acc[x][j], i);
+        };
         barrier();
-        fetch(0, lds, 0);
+        if (nk > 0) fetch(0, lds, 0);
         for (int kc = 0; kc < nk; ++kc) {
             const char *cur = lds + (kc & 1) * kBytes;
             const char *next = lds + (~kc & 1) * kBytes;
@@ -373,54 +375,258 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void linear_kernel(LinearCall c) {
             wait_first<0>();
             barrier();
             if (kc + 1 < nk) fetch(0, next, 0);
-            if (kc + 2 < nk) issue(kc + 2, kc & 1);
+            if (kc + 2 < nk) issue(kc + 2);
             multiply(1);
         }
     }
-    // 32x32 results: lane holds row lane % 32; register i column 8 (i / 4) + 4 (lane / 32) +
-    // i % 4, so four consecutive columns at a time.
-    const int lane = threadIdx.x & 63;
+
+    // Stores of a wave per 32 x 32 results, 16 bytes a lane each.
+    static constexpr int kStores = 16 * kOutSize / 16;
+
+    // What follows the product, and the stores. 32x32 results: lane holds row lane % 32;
+    // register i column 8 (i / 4) + 4 (lane / 32) + i % 4. kNT and kNN exchange halves between
+    // the half waves, so that a lane has eight neighbouring columns. Lanes outside the
+    // result store to nowhere, so that every wave issues the same number of stores.
+    template <int X>
+    __device__ void finish(const Tile &d, f32x16_t (&acc)[X][TN]) const {
+        const int half = lane >> 5;
+        char *out = static_cast<char *>(c.out) +
+                    ((kForm == kTN ? (int64_t)d.e * c.O * c.K : 0) + (int64_t)d.m0 * cols) * kOutSize;
+        const __amdgpu_buffer_rsrc_t rsrc =
+            __builtin_amdgcn_make_buffer_rsrc(out, 0, 0x7fffffff, 0x00020000);
 #pragma unroll
-    for (int x = 0; x < TM; ++x) {
-        const int m = m0 + 32 * (wm * TM + x) + (lane & 31);
-        if (m >= m_end) continue;
+        for (int x = 0; x < X; ++x) {
+            const int r = 32 * (wm + WM * x) + (lane & 31);
+            const bool row_in = d.m0 + r < d.m_end;
 #pragma unroll
-        for (int j = 0; j < TN; ++j)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int n = n0 + 32 * (wn * TN + j) + 8 * q + 4 * (lane >> 5);
-                if (n >= cols) continue;
-                float v[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) v[i] = acc[x][j][4 * q + i];
-                const int64_t at = (int64_t)m * cols + n;
+            for (int j = 0; j < TN; ++j) {
+                const int nj = d.n0 + 32 * (wn * TN + j);
                 if constexpr (kForm == kTN) {
-                    *reinterpret_cast<float4 *>(static_cast<float *>(c.out) +
-                                                (int64_t)e * c.O * c.K + at) =
-                        make_float4(v[0], v[1], v[2], v[3]);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const int n = nj + 8 * q + 4 * half;
+                        const uint32_t at = ((uint32_t)r * cols + n) * 4;
+                        const u32x4_t v = {__float_as_uint(acc[x][j][4 * q]),
+                                           __float_as_uint(acc[x][j][4 * q + 1]),
+                                           __float_as_uint(acc[x][j][4 * q + 2]),
+                                           __float_as_uint(acc[x][j][4 * q + 3])};
+                        __builtin_amdgcn_raw_buffer_store_b128(
+                            v, rsrc, (int)(row_in && n < cols ? at : kNowhere), 0, 0);
+                    }
                 } else {
-                    float u[4];
-                    if (kForm == kNT && c.bias != nullptr) {
-                        load4<In>(c.bias, (int64_t)e * c.O + n, u);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) v[i] += u[i];
-                    }
-                    if (kForm == kNT && c.relu) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) v[i] = v[i] < 0.0f ? 0.0f : v[i];
-                    }
-                    if (c.extra != nullptr) {
-                        load4<In>(c.extra, at, u);
+                    for (int p = 0; p < 2; ++p) {
+                        float v[8];
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            if (kForm == kNT) v[i] += u[i];
-                            else v[i] = u[i] > 0.0f ? v[i] : 0.0f;
+                            typedef unsigned u32x2_t __attribute__((ext_vector_type(2)));
+                            const u32x2_t w = __builtin_bit_cast(
+                                u32x2_t, __builtin_amdgcn_permlane32_swap(
+                                             __float_as_uint(acc[x][j][8 * p + i]),
+                                             __float_as_uint(acc[x][j][8 * p + 4 + i]), false, false));
+                            v[i] = __uint_as_float(w[0]);
+                            v[4 + i] = __uint_as_float(w[1]);
+                        }
+                        const int n = nj + 16 * p + 8 * half;
+                        const bool in = row_in && n < cols;
+                        const int64_t at = (int64_t)(d.m0 + r) * cols + n;
+                        if (kForm == kNT && c.bias != nullptr) {
+                            float u[8];
+                            load8<In>(c.bias, (int64_t)d.e * c.O + (n < cols ? n : 0), u);
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) v[i] += u[i];
+                        }
+                        if (kForm == kNT && c.relu) {
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) v[i] = v[i] < 0.0f ? 0.0f : v[i];
+                        }
+                        if (c.extra != nullptr) {
+                            float u[8];
+                            load8<In>(c.extra, in ? at : (int64_t)d.m0 * cols, u);
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                if (kForm == kNT) v[i] += u[i];
+                                else v[i] = u[i] > 0.0f ? v[i] : 0.0f;
+                            }
+                        }
+                        const uint32_t to = ((uint32_t)r * cols + n) * kOutSize;
+                        if constexpr (In::kBf16) {
+                            __builtin_amdgcn_raw_buffer_store_b128(RowChunk<true>::narrow(v), rsrc,
+                                                                   (int)(in ? to : kNowhere), 0, 0);
+                        } else {
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                const float w[4] = {v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]};
+                                __builtin_amdgcn_raw_buffer_store_b128(
+                                    RowChunk<false>::narrow(w), rsrc,
+                                    (int)(in ? to + 16 * h : kNowhere), 0, 0);
+                            }
                         }
                     }
-                    store4<In>(c.out, at, v);
                 }
             }
+        }
     }
+
+    // The tile that is set, then, when next is given, its first loads, which run beside the
+    // results' stores. Vector memory operations complete in order, so chunk 0 of the next
+    // tile has landed once no more are in flight than were issued behind it.
+    template <int X>
+    __device__ void compute(const Tile *next) {
+        f32x16_t acc[X][TN];
+        contract<X>(acc);
+        const Tile done = t;
+        if (next != nullptr) {
+            set(*next);
+            issue_first();
+            asm volatile("" ::: "memory");
+        }
+        finish<X>(done, acc);
+        if (next != nullptr) {
+            asm volatile("" ::: "memory");
+            constexpr int kBehind = X * TN * kStores;
+            if (nk > 1) wait_first<kLoads + kBehind>();
+            else wait_first<kBehind>();
+        }
+    }
+    __device__ void run(const Tile *next) {
+        const int rows = t.m_end - t.m0;
+        if (TM == 1 || rows > 32 * WM * (TM - 1)) compute<TM>(next);
+        else if (TM <= 2 || rows > 32 * WM * (TM - 2)) compute<(TM > 1 ? TM - 1 : 1)>(next);
+        else if (TM <= 3 || rows > 32 * WM * (TM - 3)) compute<(TM > 2 ? TM - 2 : 1)>(next);
+        else compute<(TM > 3 ? TM - 3 : 1)>(next);
+    }
+};
+
+// Tile i of kTN: every expert's tiles are spread over the XCDs (an expert with many rows
+// would else hold up one of them), a run to each. Small matrices go round by block.
+template <int BM, int BN>
+__device__ inline bool matrix_tile(const LinearCall &c, int i, Tile &t, bool &more) {
+    const int nm = (c.O + BM - 1) / BM, nn = (c.K + BN - 1) / BN, all = nm * nn;
+    int k;
+    if (all >= 32) {
+        const int per = (all + 7) / 8;
+        const int u = (blockIdx.x >> 3) + i * (gridDim.x >> 3);
+        t.e = u / per;
+        k = (blockIdx.x & 7) * per + u - t.e * per;
+    } else {
+        const int u = blockIdx.x + i * gridDim.x;
+        t.e = u / all;
+        k = u - t.e * all;
+    }
+    more = t.e < c.E;
+    if (!more || k >= all) return false;
+    int m, n;
+    tile_in_strip(k, nm, nn, m, n);
+    t.m0 = m * BM;
+    t.m_end = c.O;
+    t.n0 = n * BN;
+    t.s0 = row_bound(c.offsets, t.e, c.N);
+    t.s1 = row_bound(c.offsets, t.e + 1, c.N);
+    if (t.s1 < t.s0) t.s1 = t.s0;
+    return true;
+}
+
+// One block per compute unit, each going through its tiles: for the tile that fills a unit.
+template <class In, int kForm, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN, 1) void linear_wide_kernel(LinearCall c) {
+    using G = Tiles<In, kForm, BM, BN, WM, WN>;
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    G g(c, lds);
+    // first[e]: row tiles of the experts before e; a thread for a run of experts.
+    int32_t *first = reinterpret_cast<int32_t *>(lds + 2 * G::kBytes);   // [E + 1]
+    const int nn = (g.cols + BN - 1) / BN;
+    if constexpr (kForm != kTN) {
+        __shared__ int wave_sum[WM * WN];
+        const int per = (c.E + G::kThreads - 1) / G::kThreads;
+        const int e0 = threadIdx.x * per;
+        int sum = 0;
+        for (int e = e0; e < e0 + per && e < c.E; ++e) {
+            const int a = row_bound(c.offsets, e, c.N), z = row_bound(c.offsets, e + 1, c.N);
+            sum += z > a ? (z - a + BM - 1) / BM : 0;
+        }
+        int scan = sum;
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+            const int o = __shfl_up(scan, off);
+            if (g.lane >= off) scan += o;
+        }
+        if (g.lane == 63) wave_sum[threadIdx.x >> 6] = scan;
+        __syncthreads();
+        int at = scan - sum;
+        for (int w = 0; w < (int)(threadIdx.x >> 6); ++w) at += wave_sum[w];
+        for (int e = e0; e < e0 + per && e < c.E; ++e) {
+            const int a = row_bound(c.offsets, e, c.N), z = row_bound(c.offsets, e + 1, c.N);
+            first[e] = at;
+            at += z > a ? (z - a + BM - 1) / BM : 0;
+            if (e == c.E - 1) first[c.E] = at;
+        }
+        __syncthreads();
+    }
+    int i = 0;
+    auto next_tile = [&](Tile &t) {
+        if constexpr (kForm == kTN) {
+            bool more = true;
+            while (more)
+                if (matrix_tile<BM, BN>(c, i++, t, more)) return true;
+            return false;
+        } else {
+            const int tiles = __builtin_amdgcn_readfirstlane(first[c.E]) * nn;
+            const int k = tile_of_block(tiles, i++);
+            if (k < 0) return false;
+            int e = 0;
+            for (int e1 = 0; e1 < c.E; e1 += 64) {
+                const int q = e1 + g.lane;
+                e += __popcll(__ballot(q < c.E && first[q < c.E ? q + 1 : c.E] * nn <= k));
+            }
+            const int f = __builtin_amdgcn_readfirstlane(first[e]);
+            const int nm = __builtin_amdgcn_readfirstlane(first[e + 1]) - f;
+            int m, n;
+            tile_in_strip(k - f * nn, nm, nn, m, n);
+            t.e = e;
+            t.m0 = row_bound(c.offsets, e, c.N) + m * BM;
+            t.m_end = row_bound(c.offsets, e + 1, c.N);
+            t.n0 = n * BN;
+            t.s0 = 0;
+            t.s1 = kForm == kNT ? c.K : c.O;
+            return true;
+        }
+    };
+    Tile t, u;
+    if (!next_tile(t)) return;
+    g.set(t);
+    g.issue_first();
+    if (g.nk > 1) wait_first<G::kLoads>();
+    else wait_first<0>();
+    for (;;) {
+        const bool more = next_tile(u);
+        g.run(more ? &u : nullptr);
+        if (!more) break;
+    }
+}
+
+// One tile per block: smaller tiles, of which several share a compute unit.
+template <class In, int kForm, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN) void linear_kernel(LinearCall c) {
+    using G = Tiles<In, kForm, BM, BN, WM, WN>;
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    G g(c, lds);
+    Tile t;
+    if constexpr (kForm == kTN) {
+        bool more;
+        if (!matrix_tile<BM, BN>(c, 0, t, more)) return;
+    } else {
+        const int nn = (g.cols + BN - 1) / BN;
+        RowTile rt;
+        const int k = tile_of_block(count_row_tiles(c.offsets, c.E, c.N, BM) * nn, 0);
+        if (k < 0 || !find_row_tile(c.offsets, c.E, c.N, BM, k / nn, rt)) return;
+        t = Tile{rt.e, rt.r0, rt.r1, k % nn * BN, 0, kForm == kNT ? c.K : c.O};
+    }
+    g.set(t);
+    g.issue_first();
+    if (g.nk > 1) wait_first<G::kLoads>();
+    else wait_first<0>();
+    g.run(nullptr);
 }
 
 // db_e: column sums of dy over each expert's rows. A block for 128 bytes of an expert's
@@ -460,38 +666,57 @@ __global__ __launch_bounds__(256) void row_sums_kernel(const void *__restrict__ 
     }
 }
 
-template <class In, int kForm, int BM, int BN, int WM, int WN>
+template <class In, int kForm, int BM, int BN, int WM, int WN, bool kWide>
 hipError_t launch_tiles(const LinearCall &c, hipStream_t s) {
-    constexpr size_t kLds = 2 * (size_t)(BM + BN) * kChunk;
-    const auto kernel = &linear_kernel<In, kForm, BM, BN, WM, WN>;
-    if constexpr (kLds > 65536) {   // opted in once per device
+    const size_t lds = 2 * (size_t)(BM + BN) * kChunk + (kWide ? (size_t)(c.E + 1) * 4 : 0);
+    const void *kernel;
+    if constexpr (kWide) kernel = (const void *)&linear_wide_kernel<In, kForm, BM, BN, WM, WN>;
+    else kernel = (const void *)&linear_kernel<In, kForm, BM, BN, WM, WN>;
+    if (2 * (BM + BN) * kChunk > 65536 || kWide) {   // opted in once per device
         static std::mutex m;
         static bool granted[64] = {};
         int dev = 0;
         if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return hipErrorInvalidDevice;
         std::lock_guard<std::mutex> lock(m);
         if (!granted[dev]) {
-            const hipError_t err =
-                hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
-                                    hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLds);
+            const hipError_t err = hipFuncSetAttribute(
+                kernel, hipFuncAttributeMaxDynamicSharedMemorySize, 2 * (BM + BN) * kChunk + 2049 * 4);
             if (err != hipSuccess) return err;
             granted[dev] = true;
         }
     }
-    const int64_t nn = ((kForm == kNT ? c.O : c.K) + BN - 1) / BN;
-    const int64_t nm = kForm == kTN ? (int64_t)c.E * ((c.O + BM - 1) / BM)
-                                    : (int64_t)c.N / BM + (c.E < c.N ? c.E : c.N);
-    const int64_t blocks = (nm * nn + 7) / 8 * 8;
-    if (blocks * 64 * WM * WN >= (int64_t)1 << 32) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(64 * WM * WN), kLds, s, c);
-    return hipGetLastError();
+    int64_t blocks = kUnitsOfDevice;
+    if (!kWide) {
+        const int64_t nn = ((kForm == kNT ? c.O : c.K) + BN - 1) / BN;
+        const int64_t nm = (c.O + BM - 1) / BM;
+        if (kForm != kTN) blocks = nn * ((int64_t)c.N / BM + (c.E < c.N ? c.E : c.N));
+        else blocks = nm * nn >= 32 ? (nm * nn + 7) / 8 * 8 * c.E : nm * nn * c.E;
+        blocks = (blocks + 7) / 8 * 8;
+        if (blocks * 64 * WM * WN >= (int64_t)1 << 32) return hipErrorInvalidConfiguration;
+    }
+    LinearCall call = c;
+    void *args[] = {&call};
+    return hipLaunchKernel(kernel, dim3((unsigned)blocks), dim3(64 * WM * WN), args, lds, s);
+}
+
+template <class In, int kForm>
+hipError_t launch_form(const LinearCall &c, hipStream_t s) {
+    const int64_t avg = c.N / c.E;
+    if constexpr (!In::kBf16) {
+        if (kForm == kTN || avg >= 48) return launch_tiles<F32, kForm, 64, 128, 2, 2, false>(c, s);
+        if constexpr (kForm != kTN) return launch_tiles<F32, kForm, 32, 128, 1, 4, false>(c, s);
+    } else {
+        if (kForm == kTN || avg >= 256)
+            return launch_tiles<Bf16, kForm, 256, 256, 2, 4, true>(c, s);
+        if (avg >= 96) return launch_tiles<Bf16, kForm, 128, 128, 2, 2, false>(c, s);
+        return launch_tiles<Bf16, kForm, 64, 128, 2, 2, false>(c, s);
+    }
+    return hipErrorInvalidConfiguration;
 }
 
 template <int kForm>
-hipError_t launch_form(const LinearCall &c, int bf16, hipStream_t s) {
-    if (!bf16) return launch_tiles<F32, kForm, 128, 128, 2, 2>(c, s);
-    if (kForm == kTN || c.N >= 128 * c.E) return launch_tiles<Bf16, kForm, 256, 256, 4, 2>(c, s);
-    return launch_tiles<Bf16, kForm, 64, 128, 2, 2>(c, s);
+hipError_t launch(const LinearCall &c, int bf16, hipStream_t s) {
+    return bf16 ? launch_form<Bf16, kForm>(c, s) : launch_form<F32, kForm>(c, s);
 }
 
 }  // namespace
@@ -499,21 +724,21 @@ hipError_t launch_form(const LinearCall &c, int bf16, hipStream_t s) {
 hipError_t launch_linear(const void *x, const void *w, const void *bias, const void *residual,
                          const int32_t *offsets, void *y, int64_t N, int64_t E, int64_t K,
                          int64_t O, int relu, int bf16, hipStream_t s) {
-    return launch_form<kNT>({x, w, bias, residual, offsets, y, (int)N, (int)E, (int)K, (int)O, relu},
+    return launch<kNT>({x, w, bias, residual, offsets, y, (int)N, (int)E, (int)K, (int)O, relu},
                             bf16, s);
 }
 
 hipError_t launch_linear_dx(const void *dy, const void *w, const void *relu_of,
                             const int32_t *offsets, void *dx, int64_t N, int64_t E, int64_t K,
                             int64_t O, int bf16, hipStream_t s) {
-    return launch_form<kNN>({dy, w, nullptr, relu_of, offsets, dx, (int)N, (int)E, (int)K, (int)O, 0},
+    return launch<kNN>({dy, w, nullptr, relu_of, offsets, dx, (int)N, (int)E, (int)K, (int)O, 0},
                             bf16, s);
 }
 
 hipError_t launch_linear_dw(const void *dy, const void *x, const int32_t *offsets, float *dw,
                             float *db, int64_t N, int64_t E, int64_t K, int64_t O, int bf16,
                             hipStream_t s) {
-    const hipError_t err = launch_form<kTN>(
+    const hipError_t err = launch<kTN>(
         {dy, x, nullptr, nullptr, offsets, dw, (int)N, (int)E, (int)K, (int)O, 0}, bf16, s);
     if (err != hipSuccess || db == nullptr) return err;
     const dim3 grid((unsigned)((O * (bf16 ? 2 : 4) + 127) / 128), (unsigned)E);
