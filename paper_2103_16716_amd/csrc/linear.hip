@@ -269,7 +269,7 @@ struct Tile {
 // 32 rows and TN x 32 neighbouring columns, so that a tile with few rows left (the end of an
 // expert) is spread over the waves, which skip what lies behind: the loop is compiled for
 // each number of 32 rows a wave may have.
-template <class In, int kForm, int BM, int BN, int WM, int WN>
+template <class In, int kForm, int BM, int BN, int WM, int WN, int kStages>
 struct Tiles {
     using unit_t = typename In::unit_t;
     using elem_t = typename In::elem_t;
@@ -315,8 +315,8 @@ struct Tiles {
         B += kForm == kTN ? t.s0 * ldb + t.n0 * kSize : kForm == kNN ? t.n0 * kSize : t.n0 * ldb;
         nk = (t.s1 - t.s0 + S - 1) / S;
     }
-    __device__ void issue(int kc) const {
-        BASE_LDS char *base = (BASE_LDS char *)lds + (kc & 1) * kBytes;
+    __device__ void issue(int kc, int st) const {
+        BASE_LDS char *base = (BASE_LDS char *)lds + st * kBytes;
         const int left = t.s1 - t.s0 - kc * S;   // steps from this chunk on
         const int steps = left < S ? left : S;
         const int rows = t.m_end - t.m0 < BM ? t.m_end - t.m0 : BM;
@@ -328,14 +328,20 @@ struct Tiles {
         sb.load(B + kc * step_b, (uint32_t)end_b, left, base + StageA::kBytes);
     }
     __device__ void issue_first() const {
-        if (nk > 0) issue(0);
-        if (nk > 1) issue(1);
+#pragma unroll
+        for (int k = 0; k < kStages; ++k)
+            if (k < nk) issue(k, k);
+    }
+
+    __device__ void wait_chunk_0() const {
+        if (nk >= kStages) wait_first<kLoads * (kStages - 1)>();
+        else wait_first<0>();
     }
 
     // The products of the tile, whose first chunks have been issued and whose chunk 0 has
-    // landed for this wave. Two stages. The last quarter of a chunk is multiplied behind the
+    // landed for this wave. The last quarter of a chunk is multiplied behind the
     // barrier that hands its stage over: its operands are in registers by then, and the
-    // next chunk's first ones are read beside it. Behind the last barrier both stages are free.
+    // next chunk's first ones are read beside it. Behind the last barrier all stages are free.
     template <int X>
     __device__ void contract(f32x16_t (&acc)[X][TN]) const {
 #pragma unroll
@@ -363,20 +369,24 @@ struct Tiles {
         };
         barrier();
         if (nk > 0) fetch(0, lds, 0);
+        int st = 0;
         for (int kc = 0; kc < nk; ++kc) {
-            const char *cur = lds + (kc & 1) * kBytes;
-            const char *next = lds + (~kc & 1) * kBytes;
+            const char *cur = lds + st * kBytes;
+            const int st1 = st + 1 < kStages ? st + 1 : 0;
             fetch(1, cur, 1);
             multiply(0);
             fetch(0, cur, 2);
             multiply(1);
             fetch(1, cur, 3);
             multiply(0);
-            wait_first<0>();
+            // Chunk kc + 1 has landed once only those after it are in flight.
+            if (kc + kStages <= nk) wait_first<kLoads * (kStages - 2)>();
+            else wait_first<0>();
             barrier();
-            if (kc + 1 < nk) fetch(0, next, 0);
-            if (kc + 2 < nk) issue(kc + 2);
+            if (kc + 1 < nk) fetch(0, lds + st1 * kBytes, 0);
+            if (kc + kStages < nk) issue(kc + kStages, st);
             multiply(1);
+            st = st1;
         }
     }
 
@@ -485,7 +495,7 @@ struct Tiles {
         if (next != nullptr) {
             asm volatile("" ::: "memory");
             constexpr int kBehind = X * TN * kStores;
-            if (nk > 1) wait_first<kLoads + kBehind>();
+            if (nk >= kStages) wait_first<kLoads * (kStages - 1) + kBehind>();
             else wait_first<kBehind>();
         }
     }
@@ -528,13 +538,13 @@ __device__ inline bool matrix_tile(const LinearCall &c, int i, Tile &t, bool &mo
 }
 
 // One block per compute unit, each going through its tiles: for the tile that fills a unit.
-template <class In, int kForm, int BM, int BN, int WM, int WN>
+template <class In, int kForm, int BM, int BN, int WM, int WN, int kStages>
 __global__ __launch_bounds__(64 * WM * WN, 1) void linear_wide_kernel(LinearCall c) {
-    using G = Tiles<In, kForm, BM, BN, WM, WN>;
+    using G = Tiles<In, kForm, BM, BN, WM, WN, kStages>;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     G g(c, lds);
     // first[e]: row tiles of the experts before e; a thread for a run of experts.
-    int32_t *first = reinterpret_cast<int32_t *>(lds + 2 * G::kBytes);   // [E + 1]
+    int32_t *first = reinterpret_cast<int32_t *>(lds + kStages * G::kBytes);   // [E + 1]
     const int nn = (g.cols + BN - 1) / BN;
     if constexpr (kForm != kTN) {
         __shared__ int wave_sum[WM * WN];
@@ -596,8 +606,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void linear_wide_kernel(LinearCall
     if (!next_tile(t)) return;
     g.set(t);
     g.issue_first();
-    if (g.nk > 1) wait_first<G::kLoads>();
-    else wait_first<0>();
+    g.wait_chunk_0();
     for (;;) {
         const bool more = next_tile(u);
         g.run(more ? &u : nullptr);
@@ -606,9 +615,9 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void linear_wide_kernel(LinearCall
 }
 
 // One tile per block: smaller tiles, of which several share a compute unit.
-template <class In, int kForm, int BM, int BN, int WM, int WN>
+template <class In, int kForm, int BM, int BN, int WM, int WN, int kStages>
 __global__ __launch_bounds__(64 * WM * WN) void linear_kernel(LinearCall c) {
-    using G = Tiles<In, kForm, BM, BN, WM, WN>;
+    using G = Tiles<In, kForm, BM, BN, WM, WN, kStages>;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     G g(c, lds);
     Tile t;
@@ -624,8 +633,7 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_kernel(LinearCall c) {
     }
     g.set(t);
     g.issue_first();
-    if (g.nk > 1) wait_first<G::kLoads>();
-    else wait_first<0>();
+    g.wait_chunk_0();
     g.run(nullptr);
 }
 
@@ -666,13 +674,13 @@ __global__ __launch_bounds__(256) void row_sums_kernel(const void *__restrict__ 
     }
 }
 
-template <class In, int kForm, int BM, int BN, int WM, int WN, bool kWide>
+template <class In, int kForm, int BM, int BN, int WM, int WN, int kStages, bool kWide>
 hipError_t launch_tiles(const LinearCall &c, hipStream_t s) {
-    const size_t lds = 2 * (size_t)(BM + BN) * kChunk + (kWide ? (size_t)(c.E + 1) * 4 : 0);
+    const size_t lds = kStages * (size_t)(BM + BN) * kChunk + (kWide ? (size_t)(c.E + 1) * 4 : 0);
     const void *kernel;
-    if constexpr (kWide) kernel = (const void *)&linear_wide_kernel<In, kForm, BM, BN, WM, WN>;
-    else kernel = (const void *)&linear_kernel<In, kForm, BM, BN, WM, WN>;
-    if (2 * (BM + BN) * kChunk > 65536 || kWide) {   // opted in once per device
+    if constexpr (kWide) kernel = (const void *)&linear_wide_kernel<In, kForm, BM, BN, WM, WN, kStages>;
+    else kernel = (const void *)&linear_kernel<In, kForm, BM, BN, WM, WN, kStages>;
+    if (kStages * (BM + BN) * kChunk > 65536 || kWide) {   // opted in once per device
         static std::mutex m;
         static bool granted[64] = {};
         int dev = 0;
@@ -680,7 +688,7 @@ hipError_t launch_tiles(const LinearCall &c, hipStream_t s) {
         std::lock_guard<std::mutex> lock(m);
         if (!granted[dev]) {
             const hipError_t err = hipFuncSetAttribute(
-                kernel, hipFuncAttributeMaxDynamicSharedMemorySize, 2 * (BM + BN) * kChunk + 2049 * 4);
+                kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kStages * (BM + BN) * kChunk + 2049 * 4);
             if (err != hipSuccess) return err;
             granted[dev] = true;
         }
@@ -699,19 +707,88 @@ hipError_t launch_tiles(const LinearCall &c, hipStream_t s) {
     return hipLaunchKernel(kernel, dim3((unsigned)blocks), dim3(64 * WM * WN), args, lds, s);
 }
 
+// The choice of tile. The row ranges are on the GPU, so it goes by the rows an expert has
+// on average. A product takes the larger of one tile's time and the time of all tiles over
+// the compute units; measured us per chunk of a tile alone on a unit, and of a tile among
+// many (bf16, 64 steps a chunk; calls of N rows, E experts, K inputs, O outputs in brackets):
+//   256 x 256  1.6   1.9   (16384, 64, 1024, 4096: 215 us, 128 x 128 243, 64 x 128 311)
+//   128 x 128  0.85  0.62  (8192, 64, 1024, 4096: 155 us, 64 x 128 171, 64 x 64 202)
+//   64 x 128   0.62  0.4   (4096, 64, 1024, 4096: 127 us, 128 x 128 131, 32 x 64 182)
+//   64 x 64    0.36  0.27  (512, 1, 2048, 2048: 13.7 us, 64 x 128 22.7, 256 x 256 52)
+// The 256 x 256 tiles are one to a unit: a started round of them takes 0.4 of a whole one
+// and more. fp32 (32 steps a chunk): 64 x 128 1.03, 64 x 64 0.6, the same rate at the
+// matrix cores' limit (8192, 8, 1024, 4096: 526 us, 131 TFLOP/s, 64 x 64 571; 1501, 10, 2056,
+// 520: 77.6 and 74.0).
+struct TileCost {
+    int bm, bn;
+    double alone, many;
+};
+constexpr TileCost kCosts[] = {{64, 128, 0.62, 0.4}, {128, 128, 0.85, 0.62}, {256, 256, 1.6, 1.9},
+                               {64, 64, 0.36, 0.27}};
+
+int pick_tile(int64_t N, int64_t E, int64_t cols) {
+    const int64_t experts = E < N ? E : N;
+    int best = 0;
+    double low = 0.0;
+    for (int i = 0; i < 4; ++i) {
+        const TileCost &t = kCosts[i];
+        // Half a tile goes to waste at an expert's end.
+        double rows = (double)N / t.bm + 0.5 * experts;
+        if (rows < experts) rows = (double)experts;
+        double rounds = rows * ((cols + t.bn - 1) / t.bn) / kUnitsOfDevice;
+        if (t.bm == 256) {
+            const double whole = (double)(int64_t)rounds;
+            if (rounds > whole) rounds = whole + 0.4 + 0.6 * (rounds - whole);
+        }
+        const double cost = rounds * t.many > t.alone ? rounds * t.many : t.alone;
+        if (i == 0 || cost < low) {
+            best = i;
+            low = cost;
+        }
+    }
+    return best;
+}
+
 template <class In, int kForm>
 hipError_t launch_form(const LinearCall &c, hipStream_t s) {
     const int64_t avg = c.N / c.E;
-    if constexpr (!In::kBf16) {
-        if (kForm == kTN || avg >= 48) return launch_tiles<F32, kForm, 64, 128, 2, 2, false>(c, s);
-        if constexpr (kForm != kTN) return launch_tiles<F32, kForm, 32, 128, 1, 4, false>(c, s);
+    if constexpr (kForm == kTN) {
+        // A tile stores its matrix's part once and multiplies little, so the tile matters
+        // for experts with many rows only (64 experts, 4096 x 1024: 64 rows of 128 x 128 and
+        // 256 x 256 tiles 212 and 229 us, 8192 rows 367 and 357, 16384 rows 498 and 478).
+        if constexpr (!In::kBf16) {
+            return launch_tiles<F32, kTN, 64, 128, 2, 2, 2, false>(c, s);
+        } else {
+            const int64_t tiles = (int64_t)c.E * ((c.O + 255) / 256) * ((c.K + 255) / 256);
+            if (avg >= 96 && tiles >= 192)
+                return launch_tiles<Bf16, kTN, 256, 256, 2, 4, 2, true>(c, s);
+            return launch_tiles<Bf16, kTN, 128, 128, 2, 2, 2, false>(c, s);
+        }
+    } else if constexpr (!In::kBf16) {
+        // Few rows: as much in flight as possible (512 rows of 64 experts, 1024 to 2048: 119 us,
+        // 64 x 128 142).
+        if (avg < 32) return launch_tiles<F32, kForm, 32, 128, 1, 4, 3, false>(c, s);
+        const int64_t tiles =
+            (c.N / 64 + c.E / 2) * (((kForm == kNT ? c.O : c.K) + 127) / 128);
+        if (tiles < 4 * kUnitsOfDevice) return launch_tiles<F32, kForm, 64, 64, 2, 2, 2, false>(c, s);
+        return launch_tiles<F32, kForm, 64, 128, 2, 2, 2, false>(c, s);
     } else {
-        if (kForm == kTN || avg >= 256)
-            return launch_tiles<Bf16, kForm, 256, 256, 2, 4, true>(c, s);
-        if (avg >= 96) return launch_tiles<Bf16, kForm, 128, 128, 2, 2, false>(c, s);
-        return launch_tiles<Bf16, kForm, 64, 128, 2, 2, false>(c, s);
+        // A few rows: the matrices' bytes count, and what keeps most of them in flight (64 rows
+        // of 64 experts, 1024 to 4096: 58.6 us, 64 x 128 tiles 60.8; of 16, 2048 to 8192: 96 and
+        // 121). By columns a row of 32 x 64 tiles reads too short pieces, but for single rows.
+        if constexpr (kForm == kNT)
+            if (avg <= 16)
+                return launch_tiles<Bf16, kForm, 32, 64, 1, 2, 4, false>(c, s);
+        if constexpr (kForm == kNN)
+            if (avg <= 2)
+                return launch_tiles<Bf16, kForm, 32, 64, 1, 2, 2, false>(c, s);
+        switch (pick_tile(c.N, c.E, kForm == kNT ? c.O : c.K)) {
+            case 0: return launch_tiles<Bf16, kForm, 64, 128, 2, 2, 2, false>(c, s);
+            case 1: return launch_tiles<Bf16, kForm, 128, 128, 2, 2, 2, false>(c, s);
+            case 2: return launch_tiles<Bf16, kForm, 256, 256, 2, 4, 2, true>(c, s);
+            default: return launch_tiles<Bf16, kForm, 64, 64, 2, 2, 3, false>(c, s);
+        }
     }
-    return hipErrorInvalidConfiguration;
 }
 
 template <int kForm>
