@@ -42,7 +42,7 @@ class Routing:
 
 def _need(**tensors) -> None:
     """Every given tensor contiguous and on the current device."""
-    here = None
+    here = -1
     for name, t in tensors.items():
         if t is None:
             continue
@@ -50,14 +50,15 @@ def _need(**tensors) -> None:
             raise ValueError(f"{name} must be on the GPU")
         if not t.is_contiguous():
             raise ValueError(f"{name} must be contiguous")
-        if here is None:
-            here = _torch().cuda.current_device()
-        if t.device.index != here:
-            raise ValueError(f"{name} is on {t.device}, the current device is cuda:{here}")
+        if t.get_device() != here:
+            if here < 0:
+                here = _torch().cuda.current_device()
+            if t.get_device() != here:
+                raise ValueError(f"{name} is on {t.device}, the current device is cuda:{here}")
 
 
 def _like(name, t, shape, dtype) -> None:
-    if t is not None and (tuple(t.shape) != tuple(shape) or t.dtype != dtype):
+    if t is not None and (t.shape != shape or t.dtype != dtype):
         raise ValueError(f"{name} must be {dtype} {list(shape)}, not {t.dtype} {list(t.shape)}")
 
 
@@ -68,18 +69,18 @@ def _dims(name, t, n) -> None:
 
 def _on(stream):
     """Where outputs are allocated: the pool of the stream that writes them."""
-    return contextlib.nullcontext() if stream is None else _torch().cuda.stream(stream)
+    return _current if stream is None else _torch().cuda.stream(stream)
+
+
+_current = contextlib.nullcontext()
 
 
 def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _workspace(given, nbytes, device):
+def _workspace(nbytes, device):
     torch = _torch()
-    if given is not None:
-        _need(workspace=given)
-        return given
     return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
 
 
@@ -87,16 +88,27 @@ def topk_workspace_size(T: int, E: int, k: int) -> int:
     return int(lib().base_topk_workspace_size(T, E, k))
 
 
-def _routing(T, E, k, dev, out_perm, out_slots, out_offsets):
+def _routing(T, E, k, dev, out_perm, out_slots, out_offsets, out_assign=None, choose=False):
+    """assign (if choose), perm, slots and offsets: those given, the others cut from one
+    allocation (a small call's time is the host's)."""
     torch = _torch()
-    _need(out_perm=out_perm, out_slots=out_slots, out_offsets=out_offsets)
-    i32 = dict(dtype=torch.int32, device=dev)
-    _like("out_perm", out_perm, (T * k,), torch.int32)
-    _like("out_slots", out_slots, (T, k), torch.int32)
-    _like("out_offsets", out_offsets, (E + 1,), torch.int32)
-    return (torch.empty(T * k, **i32) if out_perm is None else out_perm,
-            torch.empty((T, k), **i32) if out_slots is None else out_slots,
-            torch.empty(E + 1, **i32) if out_offsets is None else out_offsets)
+    i32 = torch.int32
+    if out_perm is None and out_slots is None and out_offsets is None and out_assign is None:
+        n = T * k
+        buf = torch.empty((3 if choose else 2) * n + E + 1, dtype=i32, device=dev)
+        assign = buf.as_strided((T, k), (k, 1), 2 * n + E + 1) if choose else None
+        return (assign, buf.as_strided((n,), (1,), 0), buf.as_strided((T, k), (k, 1), n),
+                buf.as_strided((E + 1,), (1,), 2 * n))
+    _need(out_perm=out_perm, out_slots=out_slots, out_offsets=out_offsets, out_assign=out_assign)
+    out = []
+    for name, t, shape in (("out_assign", out_assign, (T, k)), ("out_perm", out_perm, (T * k,)),
+                           ("out_slots", out_slots, (T, k)),
+                           ("out_offsets", out_offsets, (E + 1,))):
+        if t is None and (choose or name != "out_assign"):
+            t = torch.empty(shape, dtype=i32, device=dev)
+        _like(name, t, shape, i32)
+        out.append(t)
+    return out
 
 
 def topk_assign(S, k: int, workspace=None, stream=None, out_assign=None, out_scores=None,
@@ -105,7 +117,7 @@ def topk_assign(S, k: int, workspace=None, stream=None, out_assign=None, out_sco
     index on ties, never one of score -inf or NaN; and the sort of the pairs by
     expert (base_topk_assign)."""
     torch = _torch()
-    _need(S=S, out_assign=out_assign, out_scores=out_scores)
+    _need(S=S, out_scores=out_scores, workspace=workspace)
     _dims("S", S, 2)
     if S.dtype != torch.float32:
         raise TypeError("S must be float32")
@@ -114,20 +126,20 @@ def topk_assign(S, k: int, workspace=None, stream=None, out_assign=None, out_sco
     if not 0 < k <= min(E, 64):
         raise ValueError(f"k must be in 1 .. {min(E, 64)}")
     with _on(stream):
-        _like("out_assign", out_assign, (T, k), torch.int32)
+        dev = S.device
+        assign, perm, slots, offsets = _routing(T, E, k, dev, out_perm, out_slots, out_offsets,
+                                                out_assign, True)
         _like("out_scores", out_scores, (T, k), torch.float32)
-        assign = out_assign
-        if assign is None:
-            assign = torch.empty((T, k), dtype=torch.int32, device=S.device)
         scores = out_scores
         if scores is None:
-            scores = torch.empty((T, k), dtype=torch.float32, device=S.device)
-        perm, slots, offsets = _routing(T, E, k, S.device, out_perm, out_slots, out_offsets)
-        ws = _workspace(workspace, topk_workspace_size(T, E, k), S.device)
+            scores = torch.empty((T, k), dtype=torch.float32, device=dev)
+        ws = workspace
+        if ws is None:
+            ws = _workspace(topk_workspace_size(T, E, k), dev)
         _check(lib().base_topk_assign(S.data_ptr(), T, E, k, assign.data_ptr(), scores.data_ptr(),
                                       perm.data_ptr(), slots.data_ptr(), offsets.data_ptr(),
-                                      ws.data_ptr(), ws.numel() * ws.element_size(),
-                                      _stream_ptr(stream)), "base_topk_assign")
+                                      ws.data_ptr(), ws.nbytes, _stream_ptr(stream)),
+               "base_topk_assign")
     return Routing(assign, scores, perm, slots, offsets)
 
 
@@ -136,7 +148,7 @@ def sort_by_expert(assign, E: int, workspace=None, stream=None, out_perm=None, o
     """The sort of topk_assign for given choices, int32 [T, k] (or [T]: one
     choice); entries outside [0, E) have no expert (base_sort_by_expert)."""
     torch = _torch()
-    _need(assign=assign)
+    _need(assign=assign, workspace=workspace)
     if assign.dtype != torch.int32:
         raise TypeError("assign must be int32")
     if assign.dim() == 1:
@@ -145,18 +157,21 @@ def sort_by_expert(assign, E: int, workspace=None, stream=None, out_perm=None, o
     T, k = assign.shape
     E = int(E)
     with _on(stream):
-        perm, slots, offsets = _routing(T, E, k, assign.device, out_perm, out_slots, out_offsets)
-        ws = _workspace(workspace, topk_workspace_size(T, E, k), assign.device)
+        _, perm, slots, offsets = _routing(T, E, k, assign.device, out_perm, out_slots,
+                                           out_offsets)
+        ws = workspace
+        if ws is None:
+            ws = _workspace(topk_workspace_size(T, E, k), assign.device)
         _check(lib().base_sort_by_expert(assign.data_ptr(), T, E, k, perm.data_ptr(),
                                          slots.data_ptr(), offsets.data_ptr(), ws.data_ptr(),
-                                         ws.numel() * ws.element_size(), _stream_ptr(stream)),
+                                         ws.nbytes, _stream_ptr(stream)),
                "base_sort_by_expert")
     return Routing(assign, None, perm, slots, offsets)
 
 
-def _slots_of(slots, weights):
+def _slots_of(slots, weights, **others):
     torch = _torch()
-    _need(slots=slots, weights=weights)
+    _need(slots=slots, weights=weights, **others)
     _dims("slots", slots, 2)
     if slots.dtype != torch.int32:
         raise TypeError("slots must be int32")
@@ -169,8 +184,7 @@ def dispatch(x, slots, weights=None, out=None, stream=None):
     (base_dispatch); out has T k rows. Without weights a copy bit for bit, the
     gradient of combine without weights."""
     torch = _torch()
-    T, k = _slots_of(slots, weights)
-    _need(x=x, out=out)
+    T, k = _slots_of(slots, weights, x=x, out=out)
     _dims("x", x, 2)
     d = x.shape[1]
     _like("x", x, (T, d), x.dtype)
@@ -187,8 +201,7 @@ def combine(F, slots, weights=None, residual=None, out=None, stream=None):
     """Routed rows back to their tokens, out[t] = residual[t] + sum over j of
     weights[t, j] F[slots[t, j]] (base_combine). Pairs without a row add nothing."""
     torch = _torch()
-    T, k = _slots_of(slots, weights)
-    _need(F=F, residual=residual, out=out)
+    T, k = _slots_of(slots, weights, F=F, residual=residual, out=out)
     _dims("F", F, 2)
     d = F.shape[1]
     _like("F", F, (T * k, d), F.dtype)
@@ -207,8 +220,7 @@ def combine_backward(dY, F, slots, weights, out=None, stream=None):
     """Gradient of combine with weights (base_combine_backward): (dF in routed
     order, dweights [T, k]). The residual's gradient is dY."""
     torch = _torch()
-    T, k = _slots_of(slots, weights)
-    _need(dY=dY, F=F, out=out)
+    T, k = _slots_of(slots, weights, dY=dY, F=F, out=out)
     _dims("F", F, 2)
     d = F.shape[1]
     _like("F", F, (T * k, d), F.dtype)
@@ -227,10 +239,10 @@ def combine_backward(dY, F, slots, weights, out=None, stream=None):
     return out, dw
 
 
-def _norm_args(x, weight, offsets, perm, k):
-    """(N, E, d, weight as [E, d]) of a norm's arguments."""
+def _norm_args(x, weight, offsets, perm, k, **others):
+    """(N, E, d) of a norm's arguments."""
     torch = _torch()
-    _need(x=x, weight=weight, offsets=offsets, perm=perm)
+    _need(x=x, weight=weight, offsets=offsets, perm=perm, **others)
     _dims("x", x, 2)
     d = x.shape[1]
     if weight.dim() == 1:
@@ -254,16 +266,15 @@ def expert_norm(x, weight, bias=None, offsets=None, eps: float = 1e-5, perm=None
     (y, mean, rstd). With perm, routed row r is row perm[r] // k of x. Without
     offsets one norm, weight [d] or [1, d], for every row."""
     torch = _torch()
-    N, E, d = _norm_args(x, weight, offsets, perm, k)
-    _need(bias=bias, out=out)
+    N, E, d = _norm_args(x, weight, offsets, perm, k, bias=bias, out=out)
     if bias is not None:
         _like("bias", bias, weight.shape, x.dtype)
     _like("out", out, (N, d), x.dtype)
     with _on(stream):
         if out is None:
             out = torch.empty((N, d), dtype=x.dtype, device=x.device)
-        stat = torch.empty((2, N), dtype=torch.float32, device=x.device)
-        mean, rstd = stat[0], stat[1]
+        mean = torch.empty(N, dtype=torch.float32, device=x.device)
+        rstd = torch.empty(N, dtype=torch.float32, device=x.device)
         _check(lib().base_expert_norm(x.data_ptr(), _ptr(perm), x.shape[0], k, weight.data_ptr(),
                                       _ptr(bias), _ptr(offsets), out.data_ptr(), mean.data_ptr(),
                                       rstd.data_ptr(), N, E, d, float(eps), _dtype_code(x),
@@ -280,8 +291,8 @@ def expert_norm_backward(dy, x, weight, mean, rstd, offsets=None, perm=None, k: 
     """Gradient of expert_norm (base_expert_norm_backward): (dx, dweight, dbias), dx
     in routed order with `residual` added, the others float32 of weight's shape."""
     torch = _torch()
-    N, E, d = _norm_args(x, weight, offsets, perm, k)
-    _need(dy=dy, mean=mean, rstd=rstd, residual=residual, out=out)
+    N, E, d = _norm_args(x, weight, offsets, perm, k, dy=dy, mean=mean, rstd=rstd,
+                         residual=residual, out=out, workspace=workspace)
     _like("dy", dy, (N, d), x.dtype)
     _like("mean", mean, (N,), torch.float32)
     _like("rstd", rstd, (N,), torch.float32)
@@ -290,20 +301,22 @@ def expert_norm_backward(dy, x, weight, mean, rstd, offsets=None, perm=None, k: 
     with _on(stream):
         if out is None:
             out = torch.empty((N, d), dtype=x.dtype, device=x.device)
-        sums = torch.empty((2, *weight.shape), dtype=torch.float32, device=x.device)
-        dweight, dbias = sums[0], sums[1]
-        ws = _workspace(workspace, expert_norm_workspace_size(N, E, d), x.device)
+        dweight = torch.empty(weight.shape, dtype=torch.float32, device=x.device)
+        dbias = torch.empty(weight.shape, dtype=torch.float32, device=x.device)
+        ws = workspace
+        if ws is None:
+            ws = _workspace(expert_norm_workspace_size(N, E, d), x.device)
         _check(lib().base_expert_norm_backward(
             dy.data_ptr(), x.data_ptr(), _ptr(perm), x.shape[0], k, weight.data_ptr(),
             mean.data_ptr(), rstd.data_ptr(), _ptr(offsets), _ptr(residual), out.data_ptr(),
             dweight.data_ptr(), dbias.data_ptr(), N, E, d, _dtype_code(x), ws.data_ptr(),
-            ws.numel() * ws.element_size(), _stream_ptr(stream)), "base_expert_norm_backward")
+            ws.nbytes, _stream_ptr(stream)), "base_expert_norm_backward")
     return out, dweight, dbias
 
 
-def _linear_args(w, offsets):
+def _linear_args(w, offsets, **others):
     torch = _torch()
-    _need(w=w, offsets=offsets)
+    _need(w=w, offsets=offsets, **others)
     _dims("w", w, 3)
     E, O, K = w.shape
     _like("offsets", offsets, (E + 1,), torch.int32)
@@ -315,8 +328,7 @@ def expert_linear(x, w, offsets, bias=None, relu: bool = False, residual=None, o
     """Routed rows x [N, K] times their experts' matrices w [E, O, K]: y = act(x w^T +
     bias) + residual, act the ReLU with `relu` (base_expert_linear)."""
     torch = _torch()
-    E, O, K = _linear_args(w, offsets)
-    _need(x=x, bias=bias, residual=residual, out=out)
+    E, O, K = _linear_args(w, offsets, x=x, bias=bias, residual=residual, out=out)
     _dims("x", x, 2)
     N = x.shape[0]
     _like("x", x, (N, K), w.dtype)
@@ -337,8 +349,7 @@ def expert_linear_dx(dy, w, offsets, relu_of=None, out=None, stream=None):
     """Gradient of expert_linear by its rows, dy w (base_expert_linear_dx). With relu_of
     (the ReLU's result that was x) the gradient before that ReLU: 0 where it is not > 0."""
     torch = _torch()
-    E, O, K = _linear_args(w, offsets)
-    _need(dy=dy, relu_of=relu_of, out=out)
+    E, O, K = _linear_args(w, offsets, dy=dy, relu_of=relu_of, out=out)
     _dims("dy", dy, 2)
     N = dy.shape[0]
     _like("dy", dy, (N, O), w.dtype)
