@@ -24,8 +24,7 @@ namespace {
 // Sum over the R threads (64, or a whole block of R) that share a row.
 template <int R>
 __device__ inline float row_sum(float v, float *lds) {
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off);
+    v = wave_sum(v);
     if constexpr (R > 64) {
         if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
         __syncthreads();
@@ -164,10 +163,28 @@ __global__ __launch_bounds__(kBlock<R>) void norm_backward_kernel(
             for (int q = 0; q < kN; ++q) w[c][q] = dg[c][q] = db[c][q] = 0.0f;
             if (l + c * R < ncs) Ck::widen(Ck::fetch(g, (int64_t)e * ncs + l + c * R), w[c]);
         }
+        // A row's loads are issued before the sums of the one before it.
+        u32x4_t raw_x[C], raw_dy[C];
+        int64_t src = -1;
+        float m, rs;
+        auto fetch = [&](int64_t r) {
+            src = r < z ? map.source(r) : -1;
+            if (src < 0) return;
+            m = mean[r];
+            rs = rstd[r];
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+                if (l + c * R < ncs) {
+                    raw_x[c] = Ck::fetch(x, src * ncs + l + c * R);
+                    raw_dy[c] = Ck::fetch(dy, r * ncs + l + c * R);
+                }
+        };
+        fetch(a + group);
         for (int64_t r = a + group; r < z; r += kGroups) {
-            const int64_t src = map.source(r);
-            if (src < 0) continue;   // (uniform over the threads that share the row)
-            const float m = mean[r], rs = rstd[r];
+            if (src < 0) {   // (uniform over the threads that share the row)
+                fetch(r + kGroups);
+                continue;
+            }
             float xh[C][kN], h[C][kN];
             float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
@@ -175,8 +192,8 @@ __global__ __launch_bounds__(kBlock<R>) void norm_backward_kernel(
 #pragma unroll
                 for (int q = 0; q < kN; ++q) xh[c][q] = h[c][q] = 0.0f;
                 if (l + c * R < ncs) {
-                    Ck::widen(Ck::fetch(x, src * ncs + l + c * R), xh[c]);
-                    Ck::widen(Ck::fetch(dy, r * ncs + l + c * R), h[c]);
+                    Ck::widen(raw_x[c], xh[c]);
+                    Ck::widen(raw_dy[c], h[c]);
 #pragma unroll
                     for (int q = 0; q < kN; ++q) {
                         xh[c][q] = (xh[c][q] - m) * rs;
@@ -188,6 +205,8 @@ __global__ __launch_bounds__(kBlock<R>) void norm_backward_kernel(
                     }
                 }
             }
+            const float scale = rs;
+            fetch(r + kGroups);
             s1 = row_sum<R>(s1, lds) / d;
             s2 = row_sum<R>(s2, lds) / d;
 #pragma unroll
@@ -195,7 +214,7 @@ __global__ __launch_bounds__(kBlock<R>) void norm_backward_kernel(
                 if (l + c * R >= ncs) continue;
                 float o[kN];
 #pragma unroll
-                for (int q = 0; q < kN; ++q) o[q] = rs * (h[c][q] - s1 - xh[c][q] * s2);
+                for (int q = 0; q < kN; ++q) o[q] = scale * (h[c][q] - s1 - xh[c][q] * s2);
                 if (residual != nullptr) {
                     float a[kN];
                     Ck::widen(Ck::fetch(residual, r * ncs + l + c * R), a);
@@ -243,14 +262,16 @@ __global__ __launch_bounds__(kBlock<R>) void norm_backward_kernel(
 }
 
 // dg_e and db_e: the sums of the blocks that hold rows of expert e, in their
-// order. A block for 64 of the 2 d columns of an expert; 4 waves take a quarter
-// of the blocks each.
-__global__ __launch_bounds__(256) void norm_weights_kernel(const float *__restrict__ part,
+// order. A block for 64 of the 2 d columns of an expert; its W waves take a part of
+// the blocks each: 16 where experts are few (one expert, 1024 blocks, d = 4096: 62 us with
+// four waves).
+template <int W>
+__global__ __launch_bounds__(64 * W) void norm_weights_kernel(const float *__restrict__ part,
                                                            const int32_t *__restrict__ offsets,
                                                            float *__restrict__ dg,
                                                            float *__restrict__ db, int N, int d,
                                                            int run) {
-    __shared__ float lds[4][64];
+    __shared__ float lds[W][64];
     const int e = blockIdx.y;
     const int lane = threadIdx.x & 63;
     const int wave = threadIdx.x >> 6;
@@ -260,15 +281,18 @@ __global__ __launch_bounds__(256) void norm_weights_kernel(const float *__restri
     float sum = 0.0f;
     if (a < z && i < 2 * d) {
         const int p0 = a / run, p1 = (z - 1) / run + 1;
-        const int per = (p1 - p0 + 3) / 4;
+        const int per = (p1 - p0 + W - 1) / W;
         const int q0 = p0 + wave * per;
         const int q1 = q0 + per < p1 ? q0 + per : p1;
+#pragma unroll 8
         for (int p = q0; p < q1; ++p) sum += part[((int64_t)p + e) * 2 * d + i];
     }
     lds[wave][lane] = sum;
     __syncthreads();
     if (wave == 0 && i < 2 * d) {
-        sum = (lds[0][lane] + lds[1][lane]) + (lds[2][lane] + lds[3][lane]);
+        sum = lds[0][lane];
+#pragma unroll
+        for (int w = 1; w < W; ++w) sum += lds[w][lane];
         float *out = i < d ? dg : db;
         if (out != nullptr) out[(int64_t)e * d + (i < d ? i : i - d)] = sum;
     }
@@ -300,8 +324,9 @@ void launch_norm_as(const NormCall &n, hipStream_t s) {
                        n.mean_in, n.rstd_in, n.residual, n.map, n.y, n.part, n.d);
 }
 
-// Threads per row: a wave up to 4 chunks a lane, then a block of four or sixteen.
-int row_threads(int64_t ncs) { return ncs <= 256 ? 64 : ncs <= 1024 ? 256 : 1024; }
+// Threads per row: a wave up to 4 chunks a lane, then a block of four waves, then of eight
+// (1024 threads would leave the gradient half the registers that it needs).
+int row_threads(int64_t ncs) { return ncs <= 256 ? 64 : ncs <= 1024 ? 256 : 512; }
 
 template <bool BF16>
 void launch_norm_for(const NormCall &n, hipStream_t s) {
@@ -315,8 +340,9 @@ void launch_norm_for(const NormCall &n, hipStream_t s) {
             if (ncs <= 512) return launch_norm_as<BF16, 256, 2>(n, s);
             return launch_norm_as<BF16, 256, 4>(n, s);
         default:
-            if (ncs <= 2048) return launch_norm_as<BF16, 1024, 2>(n, s);
-            return launch_norm_as<BF16, 1024, 4>(n, s);
+            if constexpr (!BF16)
+                if (ncs > 2048) return launch_norm_as<BF16, 512, 8>(n, s);
+            return launch_norm_as<BF16, 512, 4>(n, s);
     }
 }
 
@@ -324,7 +350,7 @@ int64_t rows_per_run(int64_t ncs) {
     switch (row_threads(ncs)) {
         case 64: return kRun<64>;
         case 256: return kRun<256>;
-        default: return kRun<1024>;
+        default: return kRun<512>;
     }
 }
 
@@ -376,8 +402,13 @@ hipError_t launch_norm_backward(const void *dy, const void *x, const int32_t *pe
     if (bf16) launch_norm_for<true>(n, s);
     else launch_norm_for<false>(n, s);
     const int64_t run = rows_per_run(d / (bf16 ? 8 : 4));
-    hipLaunchKernelGGL(norm_weights_kernel, dim3((unsigned)((2 * d + 63) / 64), (unsigned)E),
-                       dim3(256), 0, s, n.part, offsets, dweight, dbias, (int)N, (int)d, (int)run);
+    const dim3 grid((unsigned)((2 * d + 63) / 64), (unsigned)E);
+    if (N / run >= 32 * E)
+        hipLaunchKernelGGL(norm_weights_kernel<16>, grid, dim3(1024), 0, s, n.part, offsets, dweight,
+                           dbias, (int)N, (int)d, (int)run);
+    else
+        hipLaunchKernelGGL(norm_weights_kernel<4>, grid, dim3(256), 0, s, n.part, offsets, dweight,
+                           dbias, (int)N, (int)d, (int)run);
     return hipGetLastError();
 }
 

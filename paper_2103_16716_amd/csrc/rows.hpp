@@ -56,6 +56,27 @@ struct RowChunk {
     }
 };
 
+// Sum over the 64 lanes, in every lane: rows of 16 lanes turn by 8, 4, 2 and 1, then rows and
+// half waves are exchanged. The order is fixed. No memory is involved (a shuffle through the
+// LDS takes an order of magnitude longer).
+template <int kControl>
+__device__ inline float turned(float v) {
+    return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), kControl, 0xf, 0xf, true));
+}
+__device__ inline float wave_sum(float v) {
+    typedef unsigned u32x2_t __attribute__((ext_vector_type(2)));
+    v += turned<0x128>(v);
+    v += turned<0x124>(v);
+    v += turned<0x122>(v);
+    v += turned<0x121>(v);
+    const uint32_t a = __float_as_uint(v);
+    const u32x2_t r = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_permlane16_swap(a, a, false, false));
+    v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    const uint32_t b = __float_as_uint(v);
+    const u32x2_t h = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_permlane32_swap(b, b, false, false));
+    return __uint_as_float(h[0]) + __uint_as_float(h[1]);
+}
+
 // The experts' row ranges: expert e has rows [offsets[e], offsets[e + 1]) of N.
 // Values outside [0, N] are brought into it, so that no range leaves the
 // matrices whatever the buffer holds.
