@@ -43,7 +43,7 @@ __device__ inline bool find_row_tile(const int32_t *__restrict__ offsets, int E,
         const int e = e0 + lane;
         const int a = e < E ? row_bound(offsets, e, N) : 0;
         const int z = e < E ? row_bound(offsets, e + 1, N) : 0;
-        const int n = z > a ? (z - a + BM - 1) / BM : 0;
+        const int n = z > a ? (z - a - 1) / BM + 1 : 0;
         int sum = n;
 #pragma unroll
         for (int off = 1; off < 64; off <<= 1) {
@@ -212,7 +212,7 @@ __device__ inline int count_row_tiles(const int32_t *__restrict__ offsets, int E
     int n = 0;
     for (int e = threadIdx.x & 63; e < E; e += 64) {
         const int a = row_bound(offsets, e, N), z = row_bound(offsets, e + 1, N);
-        n += z > a ? (z - a + BM - 1) / BM : 0;
+        n += z > a ? (z - a - 1) / BM + 1 : 0;
     }
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) n += __shfl_xor(n, off);
@@ -313,7 +313,7 @@ struct Tiles {
         if (kForm != kTN) B += (int64_t)t.e * c.O * ldb;
         A += kForm == kTN ? t.s0 * lda + t.m0 * kSize : t.m0 * lda;
         B += kForm == kTN ? t.s0 * ldb + t.n0 * kSize : kForm == kNN ? t.n0 * kSize : t.n0 * ldb;
-        nk = (t.s1 - t.s0 + S - 1) / S;
+        nk = t.s1 > t.s0 ? (t.s1 - t.s0 - 1) / S + 1 : 0;
     }
     __device__ void issue(int kc, int st) const {
         BASE_LDS char *base = (BASE_LDS char *)lds + st * kBytes;
@@ -407,7 +407,7 @@ struct Tiles {
 #pragma unroll
         for (int x = 0; x < X; ++x) {
             const int r = 32 * (wm + WM * x) + (lane & 31);
-            const bool row_in = d.m0 + r < d.m_end;
+            const bool row_in = r < d.m_end - d.m0;
 #pragma unroll
             for (int j = 0; j < TN; ++j) {
                 const int nj = d.n0 + 32 * (wn * TN + j);
@@ -553,7 +553,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void linear_wide_kernel(LinearCall
         int sum = 0;
         for (int e = e0; e < e0 + per && e < c.E; ++e) {
             const int a = row_bound(c.offsets, e, c.N), z = row_bound(c.offsets, e + 1, c.N);
-            sum += z > a ? (z - a + BM - 1) / BM : 0;
+            sum += z > a ? (z - a - 1) / BM + 1 : 0;
         }
         int scan = sum;
 #pragma unroll
@@ -568,7 +568,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void linear_wide_kernel(LinearCall
         for (int e = e0; e < e0 + per && e < c.E; ++e) {
             const int a = row_bound(c.offsets, e, c.N), z = row_bound(c.offsets, e + 1, c.N);
             first[e] = at;
-            at += z > a ? (z - a + BM - 1) / BM : 0;
+            at += z > a ? (z - a - 1) / BM + 1 : 0;
             if (e == c.E - 1) first[c.E] = at;
         }
         __syncthreads();
@@ -614,27 +614,34 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void linear_wide_kernel(LinearCall
     }
 }
 
-// One tile per block: smaller tiles, of which several share a compute unit.
+// Smaller tiles, of which several share a compute unit: a block for each, or, where that
+// would be more threads than a launch may have, for some of them.
 template <class In, int kForm, int BM, int BN, int WM, int WN, int kStages>
 __global__ __launch_bounds__(64 * WM * WN) void linear_kernel(LinearCall c) {
     using G = Tiles<In, kForm, BM, BN, WM, WN, kStages>;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     G g(c, lds);
-    Tile t;
-    if constexpr (kForm == kTN) {
-        bool more;
-        if (!matrix_tile<BM, BN>(c, 0, t, more)) return;
-    } else {
-        const int nn = (g.cols + BN - 1) / BN;
-        RowTile rt;
-        const int k = tile_of_block(count_row_tiles(c.offsets, c.E, c.N, BM) * nn, 0);
-        if (k < 0 || !find_row_tile(c.offsets, c.E, c.N, BM, k / nn, rt)) return;
-        t = Tile{rt.e, rt.r0, rt.r1, k % nn * BN, 0, kForm == kNT ? c.K : c.O};
+    const int nn = (g.cols + BN - 1) / BN;
+    const int tiles = kForm == kTN ? 0 : count_row_tiles(c.offsets, c.E, c.N, BM) * nn;
+    for (int i = 0;; ++i) {
+        Tile t;
+        if constexpr (kForm == kTN) {
+            bool more;
+            if (!matrix_tile<BM, BN>(c, i, t, more)) {
+                if (!more) return;
+                continue;
+            }
+        } else {
+            RowTile rt;
+            const int k = tile_of_block(tiles, i);
+            if (k < 0 || !find_row_tile(c.offsets, c.E, c.N, BM, k / nn, rt)) return;
+            t = Tile{rt.e, rt.r0, rt.r1, k % nn * BN, 0, kForm == kNT ? c.K : c.O};
+        }
+        g.set(t);
+        g.issue_first();
+        g.wait_chunk_0();
+        g.run(nullptr);
     }
-    g.set(t);
-    g.issue_first();
-    g.wait_chunk_0();
-    g.run(nullptr);
 }
 
 // db_e: column sums of dy over each expert's rows. A block for 128 bytes of an expert's
@@ -647,30 +654,33 @@ __global__ __launch_bounds__(256) void row_sums_kernel(const void *__restrict__ 
     __shared__ float lds[32][8 * Ck::kN + 1];
     const int e = blockIdx.y;
     const int ncs = O / Ck::kN;
-    const int c = blockIdx.x * 8 + threadIdx.x % 8;
     const int g = threadIdx.x / 8;
     const int a = row_bound(offsets, e, N), z = row_bound(offsets, e + 1, N);
-    float s[Ck::kN];
+    for (int c0 = blockIdx.x * 8; c0 < ncs; c0 += gridDim.x * 8) {
+        const int c = c0 + threadIdx.x % 8;
+        float s[Ck::kN];
 #pragma unroll
-    for (int q = 0; q < Ck::kN; ++q) s[q] = 0.0f;
-    if (c < ncs) {
+        for (int q = 0; q < Ck::kN; ++q) s[q] = 0.0f;
+        if (c < ncs) {
 #pragma unroll 4
-        for (int r = a + g; r < z; r += 32) {
-            float v[Ck::kN];
-            Ck::widen(Ck::fetch(dy, (int64_t)r * ncs + c), v);
+            for (int64_t r = a + g; r < z; r += 32) {
+                float v[Ck::kN];
+                Ck::widen(Ck::fetch(dy, r * ncs + c), v);
 #pragma unroll
-            for (int q = 0; q < Ck::kN; ++q) s[q] += v[q];
+                for (int q = 0; q < Ck::kN; ++q) s[q] += v[q];
+            }
         }
-    }
 #pragma unroll
-    for (int q = 0; q < Ck::kN; ++q) lds[g][threadIdx.x % 8 * Ck::kN + q] = s[q];
-    __syncthreads();
-    const int i = threadIdx.x;
-    const int col = blockIdx.x * 8 * Ck::kN + i;
-    if (i < 8 * Ck::kN && col < O) {
-        float sum = 0.0f;
-        for (int r = 0; r < 32; ++r) sum += lds[r][i];
-        db[(int64_t)e * O + col] = sum;
+        for (int q = 0; q < Ck::kN; ++q) lds[g][threadIdx.x % 8 * Ck::kN + q] = s[q];
+        __syncthreads();
+        const int i = threadIdx.x;
+        const int col = c0 * Ck::kN + i;
+        if (i < 8 * Ck::kN && col < O) {
+            float sum = 0.0f;
+            for (int r = 0; r < 32; ++r) sum += lds[r][i];
+            db[(int64_t)e * O + col] = sum;
+        }
+        __syncthreads();
     }
 }
 
@@ -693,14 +703,14 @@ hipError_t launch_tiles(const LinearCall &c, hipStream_t s) {
             granted[dev] = true;
         }
     }
+    constexpr int64_t kMaxBlocks = 1 << 22;   // fewer than 2^32 threads
     int64_t blocks = kUnitsOfDevice;
     if (!kWide) {
         const int64_t nn = ((kForm == kNT ? c.O : c.K) + BN - 1) / BN;
         const int64_t nm = (c.O + BM - 1) / BM;
         if (kForm != kTN) blocks = nn * ((int64_t)c.N / BM + (c.E < c.N ? c.E : c.N));
         else blocks = nm * nn >= 32 ? (nm * nn + 7) / 8 * 8 * c.E : nm * nn * c.E;
-        blocks = (blocks + 7) / 8 * 8;
-        if (blocks * 64 * WM * WN >= (int64_t)1 << 32) return hipErrorInvalidConfiguration;
+        blocks = blocks < kMaxBlocks ? (blocks + 7) / 8 * 8 : kMaxBlocks;
     }
     LinearCall call = c;
     void *args[] = {&call};
@@ -818,7 +828,8 @@ hipError_t launch_linear_dw(const void *dy, const void *x, const int32_t *offset
     const hipError_t err = launch<kTN>(
         {dy, x, nullptr, nullptr, offsets, dw, (int)N, (int)E, (int)K, (int)O, 0}, bf16, s);
     if (err != hipSuccess || db == nullptr) return err;
-    const dim3 grid((unsigned)((O * (bf16 ? 2 : 4) + 127) / 128), (unsigned)E);
+    const int64_t parts = (O * (bf16 ? 2 : 4) + 127) / 128;
+    const dim3 grid((unsigned)(parts < 1024 ? parts : 1024), (unsigned)E);
     if (bf16)
         hipLaunchKernelGGL(row_sums_kernel<true>, grid, dim3(256), 0, s, dy, offsets, db, (int)N,
                            (int)O);

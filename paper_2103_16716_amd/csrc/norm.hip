@@ -69,62 +69,65 @@ __global__ __launch_bounds__(kBlock<R>) void norm_kernel(
     __shared__ float lds[16];
     const int ncs = d / Ck::kN;
     const int l = threadIdx.x % R;
-    const int64_t r = (int64_t)blockIdx.x * (kBlock<R> / R) + threadIdx.x / R;
-    if (r >= map.N) return;   // (whole rows: uniform over the threads that share one)
-    const int e = map.expert((int)r);
-    const int64_t src = map.source(r);
-    if (e < 0 || src < 0) return;
-    float v[C][Ck::kN];
-    float sum = 0.0f;
+    constexpr int kRows = kBlock<R> / R;
+    // (r, e and src are uniform over the threads that share a row.)
+    for (int64_t r = (int64_t)blockIdx.x * kRows + threadIdx.x / R; r < map.N;
+         r += (int64_t)gridDim.x * kRows) {
+        const int e = map.expert((int)r);
+        const int64_t src = map.source(r);
+        if (e < 0 || src < 0) continue;
+        float v[C][Ck::kN];
+        float sum = 0.0f;
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-        const int i = l + c * R;
+        for (int c = 0; c < C; ++c) {
+            const int i = l + c * R;
 #pragma unroll
-        for (int q = 0; q < Ck::kN; ++q) v[c][q] = 0.0f;
-        if (i < ncs) Ck::widen(Ck::fetch(x, src * ncs + i), v[c]);
-    }
-#pragma unroll
-    for (int c = 0; c < C; ++c)
-#pragma unroll
-        for (int q = 0; q < Ck::kN; ++q) sum += v[c][q];
-    const float m = row_sum<R>(sum, lds) / d;
-    float sq = 0.0f;
-#pragma unroll
-    for (int c = 0; c < C; ++c)
-        if (l + c * R < ncs)
-#pragma unroll
-            for (int q = 0; q < Ck::kN; ++q) {
-                v[c][q] -= m;
-                sq = fmaf(v[c][q], v[c][q], sq);
-            }
-    const float rs = 1.0f / sqrtf(row_sum<R>(sq, lds) / d + eps);
-    if (l == 0) {
-        mean[r] = m;
-        rstd[r] = rs;
-    }
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-        const int i = l + c * R;
-        if (i >= ncs) continue;
-        float w[Ck::kN], o[Ck::kN];
-        Ck::widen(Ck::fetch(g, (int64_t)e * ncs + i), w);
-        if (b != nullptr) {
-            Ck::widen(Ck::fetch(b, (int64_t)e * ncs + i), o);
-        } else {
-#pragma unroll
-            for (int q = 0; q < Ck::kN; ++q) o[q] = 0.0f;
+            for (int q = 0; q < Ck::kN; ++q) v[c][q] = 0.0f;
+            if (i < ncs) Ck::widen(Ck::fetch(x, src * ncs + i), v[c]);
         }
 #pragma unroll
-        for (int q = 0; q < Ck::kN; ++q) o[q] = fmaf(v[c][q] * rs, w[q], o[q]);
-        Ck::store(y, r * ncs + i, o);
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int q = 0; q < Ck::kN; ++q) sum += v[c][q];
+        const float m = row_sum<R>(sum, lds) / d;
+        float sq = 0.0f;
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+            if (l + c * R < ncs)
+#pragma unroll
+                for (int q = 0; q < Ck::kN; ++q) {
+                    v[c][q] -= m;
+                    sq = fmaf(v[c][q], v[c][q], sq);
+                }
+        const float rs = 1.0f / sqrtf(row_sum<R>(sq, lds) / d + eps);
+        if (l == 0) {
+            mean[r] = m;
+            rstd[r] = rs;
+        }
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int i = l + c * R;
+            if (i >= ncs) continue;
+            float w[Ck::kN], o[Ck::kN];
+            Ck::widen(Ck::fetch(g, (int64_t)e * ncs + i), w);
+            if (b != nullptr) {
+                Ck::widen(Ck::fetch(b, (int64_t)e * ncs + i), o);
+            } else {
+#pragma unroll
+                for (int q = 0; q < Ck::kN; ++q) o[q] = 0.0f;
+            }
+#pragma unroll
+            for (int q = 0; q < Ck::kN; ++q) o[q] = fmaf(v[c][q] * rs, w[q], o[q]);
+            Ck::store(y, r * ncs + i, o);
+        }
     }
 }
 
-// A block takes kRun<R> consecutive rows, R threads a row, and goes through the
+// A block takes runs of kRun<R> consecutive rows, R threads a row, and goes through the
 // experts that have rows among them. Each thread sums dy xh and dy of its own
 // columns over its rows; the groups of R threads add theirs in LDS one after
-// another. The sums of block p's rows of expert e go to slot p + e of the partial
-// sums: p + e grows from each (block, expert) with rows in common to the next, so
+// another. The sums of run p's rows of expert e go to slot p + e of the partial
+// sums: p + e grows from each (run, expert) with rows in common to the next, so
 // that no two share a slot.
 template <int R>
 constexpr int kRun = 16 * (kBlock<R> / R);
@@ -142,122 +145,124 @@ __global__ __launch_bounds__(kBlock<R>) void norm_backward_kernel(
     const int ncs = d / kN;
     const int l = threadIdx.x % R;
     const int group = threadIdx.x / R;
-    const int64_t r0 = (int64_t)blockIdx.x * kRun<R>;
-    const int64_t r1 = r0 + kRun<R> < map.N ? r0 + kRun<R> : map.N;
-    int e = 0;
-    if (map.offsets != nullptr) e = expert_of_row(map.offsets, map.E, (int)r0);
-    for (; e < map.E; ++e) {   // (uniform)
-        int64_t a = r0, z = r1;
-        if (map.offsets != nullptr) {
-            const int64_t ea = row_bound(map.offsets, e, map.N);
-            const int64_t ez = row_bound(map.offsets, e + 1, map.N);
-            if (ea >= r1) break;
-            a = ea > r0 ? ea : r0;
-            z = ez < r1 ? ez : r1;
-            if (a >= z) continue;
-        }
-        float w[C][kN], dg[C][kN], db[C][kN];
+    for (int64_t run = blockIdx.x; run * kRun<R> < map.N; run += gridDim.x) {
+        const int64_t r0 = run * kRun<R>;
+        const int64_t r1 = r0 + kRun<R> < map.N ? r0 + kRun<R> : map.N;
+        int e = 0;
+        if (map.offsets != nullptr) e = expert_of_row(map.offsets, map.E, (int)r0);
+        for (; e < map.E; ++e) {   // (uniform)
+            int64_t a = r0, z = r1;
+            if (map.offsets != nullptr) {
+                const int64_t ea = row_bound(map.offsets, e, map.N);
+                const int64_t ez = row_bound(map.offsets, e + 1, map.N);
+                if (ea >= r1) break;
+                a = ea > r0 ? ea : r0;
+                z = ez < r1 ? ez : r1;
+                if (a >= z) continue;
+            }
+            float w[C][kN], dg[C][kN], db[C][kN];
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
+            for (int c = 0; c < C; ++c) {
 #pragma unroll
-            for (int q = 0; q < kN; ++q) w[c][q] = dg[c][q] = db[c][q] = 0.0f;
-            if (l + c * R < ncs) Ck::widen(Ck::fetch(g, (int64_t)e * ncs + l + c * R), w[c]);
-        }
-        // A row's loads are issued before the sums of the one before it.
-        u32x4_t raw_x[C], raw_dy[C];
-        int64_t src = -1;
-        float m, rs;
-        auto fetch = [&](int64_t r) {
-            src = r < z ? map.source(r) : -1;
-            if (src < 0) return;
-            m = mean[r];
-            rs = rstd[r];
+                for (int q = 0; q < kN; ++q) w[c][q] = dg[c][q] = db[c][q] = 0.0f;
+                if (l + c * R < ncs) Ck::widen(Ck::fetch(g, (int64_t)e * ncs + l + c * R), w[c]);
+            }
+            // A row's loads are issued before the sums of the one before it.
+            u32x4_t raw_x[C], raw_dy[C];
+            int64_t src = -1;
+            float m, rs;
+            auto fetch = [&](int64_t r) {
+                src = r < z ? map.source(r) : -1;
+                if (src < 0) return;
+                m = mean[r];
+                rs = rstd[r];
 #pragma unroll
-            for (int c = 0; c < C; ++c)
-                if (l + c * R < ncs) {
-                    raw_x[c] = Ck::fetch(x, src * ncs + l + c * R);
-                    raw_dy[c] = Ck::fetch(dy, r * ncs + l + c * R);
+                for (int c = 0; c < C; ++c)
+                    if (l + c * R < ncs) {
+                        raw_x[c] = Ck::fetch(x, src * ncs + l + c * R);
+                        raw_dy[c] = Ck::fetch(dy, r * ncs + l + c * R);
+                    }
+            };
+            fetch(a + group);
+            for (int64_t r = a + group; r < z; r += kGroups) {
+                if (src < 0) {   // (uniform over the threads that share the row)
+                    fetch(r + kGroups);
+                    continue;
                 }
-        };
-        fetch(a + group);
-        for (int64_t r = a + group; r < z; r += kGroups) {
-            if (src < 0) {   // (uniform over the threads that share the row)
+                float xh[C][kN], h[C][kN];
+                float s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+                for (int c = 0; c < C; ++c) {
+#pragma unroll
+                    for (int q = 0; q < kN; ++q) xh[c][q] = h[c][q] = 0.0f;
+                    if (l + c * R < ncs) {
+                        Ck::widen(raw_x[c], xh[c]);
+                        Ck::widen(raw_dy[c], h[c]);
+#pragma unroll
+                        for (int q = 0; q < kN; ++q) {
+                            xh[c][q] = (xh[c][q] - m) * rs;
+                            dg[c][q] = fmaf(h[c][q], xh[c][q], dg[c][q]);
+                            db[c][q] += h[c][q];
+                            h[c][q] *= w[c][q];
+                            s1 += h[c][q];
+                            s2 = fmaf(h[c][q], xh[c][q], s2);
+                        }
+                    }
+                }
+                const float scale = rs;
                 fetch(r + kGroups);
-                continue;
-            }
-            float xh[C][kN], h[C][kN];
-            float s1 = 0.0f, s2 = 0.0f;
+                s1 = row_sum<R>(s1, lds) / d;
+                s2 = row_sum<R>(s2, lds) / d;
 #pragma unroll
-            for (int c = 0; c < C; ++c) {
+                for (int c = 0; c < C; ++c) {
+                    if (l + c * R >= ncs) continue;
+                    float o[kN];
 #pragma unroll
-                for (int q = 0; q < kN; ++q) xh[c][q] = h[c][q] = 0.0f;
-                if (l + c * R < ncs) {
-                    Ck::widen(raw_x[c], xh[c]);
-                    Ck::widen(raw_dy[c], h[c]);
+                    for (int q = 0; q < kN; ++q) o[q] = scale * (h[c][q] - s1 - xh[c][q] * s2);
+                    if (residual != nullptr) {
+                        float a[kN];
+                        Ck::widen(Ck::fetch(residual, r * ncs + l + c * R), a);
 #pragma unroll
-                    for (int q = 0; q < kN; ++q) {
-                        xh[c][q] = (xh[c][q] - m) * rs;
-                        dg[c][q] = fmaf(h[c][q], xh[c][q], dg[c][q]);
-                        db[c][q] += h[c][q];
-                        h[c][q] *= w[c][q];
-                        s1 += h[c][q];
-                        s2 = fmaf(h[c][q], xh[c][q], s2);
+                        for (int q = 0; q < kN; ++q) o[q] += a[q];
                     }
+                    Ck::store(dx, r * ncs + l + c * R, o);
                 }
             }
-            const float scale = rs;
-            fetch(r + kGroups);
-            s1 = row_sum<R>(s1, lds) / d;
-            s2 = row_sum<R>(s2, lds) / d;
+            float *out = part + (run + e) * 2 * d;
+            if constexpr (kGroups > 1) {
+                for (int w0 = 0; w0 < kGroups; ++w0) {
+                    if (group == w0)
 #pragma unroll
-            for (int c = 0; c < C; ++c) {
-                if (l + c * R >= ncs) continue;
-                float o[kN];
+                        for (int c = 0; c < C; ++c)
+                            if (l + c * R < ncs)
 #pragma unroll
-                for (int q = 0; q < kN; ++q) o[q] = scale * (h[c][q] - s1 - xh[c][q] * s2);
-                if (residual != nullptr) {
-                    float a[kN];
-                    Ck::widen(Ck::fetch(residual, r * ncs + l + c * R), a);
-#pragma unroll
-                    for (int q = 0; q < kN; ++q) o[q] += a[q];
+                                for (int q = 0; q < kN; ++q) {
+                                    const int i = (l + c * R) * kN + q;
+                                    if (w0 > 0) {
+                                        dg[c][q] += sums[i];
+                                        db[c][q] += sums[d + i];
+                                    }
+                                    if (w0 < kGroups - 1) {
+                                        sums[i] = dg[c][q];
+                                        sums[d + i] = db[c][q];
+                                    }
+                                }
+                    __syncthreads();
                 }
-                Ck::store(dx, r * ncs + l + c * R, o);
             }
+            if (group == kGroups - 1)
+#pragma unroll
+                for (int c = 0; c < C; ++c)
+                    if (l + c * R < ncs)
+#pragma unroll
+                        for (int q = 0; q < kN; q += 4) {
+                            const int i = (l + c * R) * kN + q;
+                            *reinterpret_cast<float4 *>(out + i) =
+                                make_float4(dg[c][q], dg[c][q + 1], dg[c][q + 2], dg[c][q + 3]);
+                            *reinterpret_cast<float4 *>(out + d + i) =
+                                make_float4(db[c][q], db[c][q + 1], db[c][q + 2], db[c][q + 3]);
+                        }
         }
-        float *out = part + ((int64_t)blockIdx.x + e) * 2 * d;
-        if constexpr (kGroups > 1) {
-            for (int w0 = 0; w0 < kGroups; ++w0) {
-                if (group == w0)
-#pragma unroll
-                    for (int c = 0; c < C; ++c)
-                        if (l + c * R < ncs)
-#pragma unroll
-                            for (int q = 0; q < kN; ++q) {
-                                const int i = (l + c * R) * kN + q;
-                                if (w0 > 0) {
-                                    dg[c][q] += sums[i];
-                                    db[c][q] += sums[d + i];
-                                }
-                                if (w0 < kGroups - 1) {
-                                    sums[i] = dg[c][q];
-                                    sums[d + i] = db[c][q];
-                                }
-                            }
-                __syncthreads();
-            }
-        }
-        if (group == kGroups - 1)
-#pragma unroll
-            for (int c = 0; c < C; ++c)
-                if (l + c * R < ncs)
-#pragma unroll
-                    for (int q = 0; q < kN; q += 4) {
-                        const int i = (l + c * R) * kN + q;
-                        *reinterpret_cast<float4 *>(out + i) =
-                            make_float4(dg[c][q], dg[c][q + 1], dg[c][q + 2], dg[c][q + 3]);
-                        *reinterpret_cast<float4 *>(out + d + i) =
-                            make_float4(db[c][q], db[c][q + 1], db[c][q + 2], db[c][q + 3]);
-                    }
     }
 }
 
@@ -298,6 +303,8 @@ __global__ __launch_bounds__(64 * W) void norm_weights_kernel(const float *__res
     }
 }
 
+constexpr int64_t kMaxBlocks = 1 << 22;   // a launch has fewer than 2^32 threads; rows go round
+
 struct NormCall {
     const void *x, *g, *b, *dy, *residual;
     const float *mean_in, *rstd_in;
@@ -312,13 +319,14 @@ struct NormCall {
 template <bool BF16, int R, int C>
 void launch_norm_as(const NormCall &n, hipStream_t s) {
     constexpr int kGroups = kBlock<R> / R;
+    const int64_t rows = n.backward ? kRun<R> : kGroups;
+    int64_t blocks = ((int64_t)n.map.N + rows - 1) / rows;
+    if (blocks > kMaxBlocks) blocks = kMaxBlocks;
     if (!n.backward) {
-        const int64_t blocks = ((int64_t)n.map.N + kGroups - 1) / kGroups;
         hipLaunchKernelGGL((norm_kernel<BF16, R, C>), dim3((unsigned)blocks), dim3(kBlock<R>), 0, s,
                            n.x, n.g, n.b, n.map, n.y, n.mean, n.rstd, n.d, n.eps);
         return;
     }
-    const int64_t blocks = ((int64_t)n.map.N + kRun<R> - 1) / kRun<R>;
     hipLaunchKernelGGL((norm_backward_kernel<BF16, R, C>), dim3((unsigned)blocks),
                        dim3(kBlock<R>), kGroups > 1 ? (size_t)n.d * 8 : 0, s, n.dy, n.x, n.g,
                        n.mean_in, n.rstd_in, n.residual, n.map, n.y, n.part, n.d);

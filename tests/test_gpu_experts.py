@@ -357,6 +357,62 @@ def test_offsets_out_of_order_stay_in_bounds():
     torch.cuda.synchronize()
 
 
+def near_product(got, a, b, terms, step):
+    """got against a b in fp64 on the GPU: a fp32 sum of so many terms, stored with `step`."""
+    a, b = a.double(), b.double()
+    want = a @ b
+    bound = (terms + 3) * U * (a.abs() @ b.abs())
+    assert bool(((got.double() - want).abs() <= bound + step * (want.abs() + bound)).all())
+
+
+def test_matrices_beyond_32_bits():
+    """More than 2^32 bytes and 2^31 elements in the rows, then in the matrices: the last
+    rows and the last expert have their results."""
+    g = torch.Generator(device="cuda").manual_seed(1)
+    N, n, K, O, E = 270000, 200, 8192, 64, 3
+    m = 130                                            # rows of expert 0; expert 2 the others
+    x = torch.empty(N, K, dtype=torch.bfloat16, device="cuda")
+    tail = torch.randn(n, K, generator=g, device="cuda").bfloat16()
+    x[N - n:] = tail
+    dy = torch.randn(N, O, generator=g, device="cuda").bfloat16()
+    dt = dy[N - n:]
+    w = (torch.randn(E, O, K, generator=g, device="cuda") * K ** -0.5).bfloat16()
+    off = torch.tensor([N - n, N - n + m, N - n + m, N], dtype=torch.int32, device="cuda")
+    y = pb.expert_linear(x, w, off)[N - n:]
+    near_product(y[:m], tail[:m], w[0].t().contiguous(), K, 2.0 ** -8)
+    near_product(y[m:], tail[m:], w[2].t().contiguous(), K, 2.0 ** -8)
+    dx = torch.empty_like(x)
+    pb.expert_linear_dx(dy, w, off, out=dx)
+    near_product(dx[N - n:N - n + m], dt[:m], w[0], O, 2.0 ** -8)
+    near_product(dx[N - n + m:], dt[m:], w[2], O, 2.0 ** -8)
+    dw = pb.expert_linear_dw(dy, x, off)[0]
+    near_product(dw[0], dt[:m].t().contiguous(), tail[:m], m, U)
+    near_product(dw[2], dt[m:].t().contiguous(), tail[m:], n - m, U)
+    assert not torch.any(dw[1])
+    gain = w[:, 0].contiguous()
+    y, mean, rstd = pb.expert_norm(x, gain, None, off, out=dx)
+    want, mean_t, _ = pb.expert_norm(tail, gain, None, off - (N - n))
+    assert torch.equal(y[N - n:], want) and torch.equal(mean[N - n:], mean_t)
+    slots = torch.full((N, 1), -1, dtype=torch.int32, device="cuda")
+    slots[N - n:, 0] = torch.arange(N - 1, N - n - 1, -1, device="cuda", dtype=torch.int32)
+    moved = pb.dispatch(x, slots, out=dx)
+    assert torch.equal(moved[N - n:], tail.flip(0))
+    back = pb.combine(moved, slots)
+    assert torch.equal(back[N - n:], tail) and not torch.any(back[0])
+    del x, dx, y, moved, back
+    E, O = 300, 1024
+    w = torch.empty(E, O, K, dtype=torch.bfloat16, device="cuda")
+    w[E - 1] = (torch.randn(O, K, generator=g, device="cuda") * K ** -0.5).bfloat16()
+    off = torch.zeros(E + 1, dtype=torch.int32, device="cuda")
+    off[E] = n
+    dy = torch.randn(n, O, generator=g, device="cuda").bfloat16()
+    near_product(pb.expert_linear(tail, w, off), tail, w[E - 1].t().contiguous(), K, 2.0 ** -8)
+    near_product(pb.expert_linear_dx(dy, w, off), dy, w[E - 1], O, 2.0 ** -8)
+    dw, db = pb.expert_linear_dw(dy, tail, off)
+    near_product(dw[E - 1], dy.t().contiguous(), tail, n, U)
+    assert not torch.any(dw[E - 2]) and not torch.any(db[:E - 1])
+
+
 # ----------------------------------------------------------------- together --
 
 def block(H, S, k, p, dOut):
