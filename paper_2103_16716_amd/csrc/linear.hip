@@ -323,7 +323,8 @@ struct Tiles {
         B += kForm == kTN ? t.s0 * ldb + t.n0 * kSize : kForm == kNN ? t.n0 * kSize : t.n0 * ldb;
         nk = t.s1 > t.s0 ? (t.s1 - t.s0 - 1) / S + 1 : 0;
     }
-    __device__ void issue(int kc, int st) const {
+    // The loads of chunk kc into stage st, of operand A (1), B (2) or both.
+    __device__ void issue(int kc, int st, int which) const {
         BASE_LDS char *base = (BASE_LDS char *)lds + st * kBytes;
         const int left = t.s1 - t.s0 - kc * S;   // steps from this chunk on
         const int steps = left < S ? left : S;
@@ -332,24 +333,46 @@ struct Tiles {
         const int64_t step_b = kForm == kNT ? kChunk : S * ldb;
         const int64_t end_a = kForm == kTN ? steps * lda - t.m0 * kSize : rows * lda - kc * kChunk;
         const int64_t end_b = kForm == kNT ? ncols * ldb - kc * kChunk : steps * ldb - t.n0 * kSize;
-        sa.load(A + kc * step_a, (uint32_t)end_a, left, base);
-        sb.load(B + kc * step_b, (uint32_t)end_b, left, base + StageA::kBytes);
+        if (which & 1) sa.load(A + kc * step_a, (uint32_t)end_a, left, base);
+        if (which & 2) sb.load(B + kc * step_b, (uint32_t)end_b, left, base + StageA::kBytes);
     }
     __device__ void issue_first() const {
 #pragma unroll
         for (int k = 0; k < kStages; ++k)
-            if (k < nk) issue(k, k);
+            if (k < nk) issue(k, k, 3);
     }
 
+    // Operand reads go between the products of the step before, one to a product or every
+    // few: 32768 rows x 2048 to 8192, 32 experts 1035 -> 1010 us, by columns 1028 -> 1005. (Not for
+    // the matrices' gradient: 4096 rows of 64 experts, 1024 to 4096, 274 -> 306 us.)
+    template <int X>
+    __device__ static void interleave() {
+        if constexpr (In::kBf16 && kForm != kTN) {
+            constexpr int reads = X + TN * (kForm == kNT ? 1 : 2);
+            constexpr int every = X * TN / reads > 0 ? X * TN / reads : 1;
+            constexpr int per = (reads * every + X * TN - 1) / (X * TN);
+#pragma unroll
+            for (int i = 0; i < X * TN / every; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x8, every, 0);   // matrix instructions
+                __builtin_amdgcn_sched_group_barrier(0x100, per, 0);   // LDS reads
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
     __device__ void wait_chunk_0() const {
         if (nk >= kStages) wait_first<kLoads * (kStages - 1)>();
         else wait_first<0>();
     }
 
     // The products of the tile, whose first chunks have been issued and whose chunk 0 has
-    // landed for this wave. The last quarter of a chunk is multiplied behind the
-    // barrier that hands its stage over: its operands are in registers by then, and the
-    // next chunk's first ones are read beside it. Behind the last barrier all stages are free.
+    // landed for this wave. The last quarter of a chunk is multiplied behind the barrier that
+    // hands its stage over: its operands are in registers by then, and the next chunk's
+    // first ones are read beside it. Behind the last barrier all stages are free.
+    // 256 x 256 tiles load into the stage handed over in two parts, A behind the barrier and B
+    // a quarter of a chunk later (both at once: 32768 rows x 2048 to 8192, 32 experts 1010 us,
+    // 975 so; smaller tiles are bound by the loads and issue them at once: 8192 rows by columns
+    // of 64 experts, 4096 to 1024, 209 us in two parts, 164 at once).
+    static constexpr bool kSplit = BM == 256 && kStages == 2;
     template <int X>
     __device__ void contract(f32x16_t (&acc)[X][TN]) const {
 #pragma unroll
@@ -382,18 +405,23 @@ struct Tiles {
             const char *cur = lds + st * kBytes;
             const int st1 = st + 1 < kStages ? st + 1 : 0;
             fetch(1, cur, 1);
+            if (kSplit && kc > 0 && kc + 1 < nk) issue(kc + 1, st1, 2);
             multiply(0);
+            interleave<X>();
             fetch(0, cur, 2);
             multiply(1);
+            interleave<X>();
             fetch(1, cur, 3);
             multiply(0);
+            interleave<X>();
             // Chunk kc + 1 has landed once only those after it are in flight.
             if (kc + kStages <= nk) wait_first<kLoads * (kStages - 2)>();
             else wait_first<0>();
             barrier();
             if (kc + 1 < nk) fetch(0, lds + st1 * kBytes, 0);
-            if (kc + kStages < nk) issue(kc + kStages, st);
+            if (kc + kStages < nk) issue(kc + kStages, st, kSplit ? 1 : 3);
             multiply(1);
+            if (In::kBf16 && kForm != kTN) __builtin_amdgcn_sched_barrier(0);
             st = st1;
         }
     }
@@ -581,6 +609,8 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void linear_wide_kernel(LinearCall
         }
         __syncthreads();
     }
+    // An XCD's tiles go round its blocks. Those of a last round that would leave half of the
+    // blocks without one are cut into two or four by their rows.
     int i = 0;
     auto next_tile = [&](Tile &t) {
         if constexpr (kForm == kTN) {
@@ -590,21 +620,42 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void linear_wide_kernel(LinearCall
             return false;
         } else {
             const int tiles = __builtin_amdgcn_readfirstlane(first[c.E]) * nn;
-            const int k = tile_of_block(tiles, i++);
-            if (k < 0) return false;
-            int e = 0;
-            for (int e1 = 0; e1 < c.E; e1 += 64) {
-                const int q = e1 + g.lane;
-                e += __popcll(__ballot(q < c.E && first[q < c.E ? q + 1 : c.E] * nn <= k));
+            const int run = (tiles + 7) / 8;
+            const int left = tiles - (blockIdx.x & 7) * run;
+            const int mine = left < run ? left : run;   // (may be negative)
+            const int slots = gridDim.x >> 3;
+            const int whole = mine > 0 ? mine / slots * slots : 0;
+            const int rest = mine - whole;
+            const int parts = 4 * rest <= slots ? 4 : 2 * rest <= slots ? 2 : 1;
+            for (;;) {
+                int u = (blockIdx.x >> 3) + slots * i++;
+                int part = 0, rows = BM;
+                if (u >= whole) {
+                    u -= whole;
+                    if (u >= rest * parts) return false;
+                    part = u % parts;
+                    rows = BM / parts;
+                    u = whole + u / parts;
+                }
+                const int k = (blockIdx.x & 7) * run + u;
+                int e = 0;
+                for (int e1 = 0; e1 < c.E; e1 += 64) {
+                    const int q = e1 + g.lane;
+                    e += __popcll(__ballot(q < c.E && first[q < c.E ? q + 1 : c.E] * nn <= k));
+                }
+                const int f = __builtin_amdgcn_readfirstlane(first[e]);
+                const int a = row_bound(c.offsets, e, c.N);
+                t.e = e;
+                t.m_end = row_bound(c.offsets, e + 1, c.N);
+                int m, n;
+                const int nm = __builtin_amdgcn_readfirstlane(first[e + 1]) - f;
+                tile_in_strip(k - f * nn, nm, nn, m, n);
+                t.m0 = a + m * BM + part * rows;
+                if (t.m0 >= t.m_end) continue;
+                if (t.m_end - t.m0 > rows) t.m_end = t.m0 + rows;
+                t.n0 = n * BN;
+                break;
             }
-            const int f = __builtin_amdgcn_readfirstlane(first[e]);
-            const int nm = __builtin_amdgcn_readfirstlane(first[e + 1]) - f;
-            int m, n;
-            tile_in_strip(k - f * nn, nm, nn, m, n);
-            t.e = e;
-            t.m0 = row_bound(c.offsets, e, c.N) + m * BM;
-            t.m_end = row_bound(c.offsets, e + 1, c.N);
-            t.n0 = n * BN;
             t.s0 = 0;
             t.s1 = kForm == kNT ? c.K : c.O;
             return true;
@@ -733,8 +784,8 @@ hipError_t launch_tiles(const LinearCall &c, hipStream_t s) {
 //   128 x 128  0.85  0.62  (8192, 64, 1024, 4096: 155 us, 64 x 128 171, 64 x 64 202)
 //   64 x 128   0.62  0.4   (4096, 64, 1024, 4096: 127 us, 128 x 128 131, 32 x 64 182)
 //   64 x 64    0.36  0.27  (512, 1, 2048, 2048: 13.7 us, 64 x 128 22.7, 256 x 256 52)
-// The 256 x 256 tiles are one to a unit: a started round of them takes 0.4 of a whole one
-// and more. fp32 (32 steps a chunk): 64 x 128 1.03, 64 x 64 0.6, the same rate at the
+// The 256 x 256 tiles are one to a unit: a started round of them takes a whole one's time,
+// or 0.6 or 0.4 of it where its tiles are cut. fp32 (32 steps a chunk): 64 x 128 1.03, 64 x 64 0.6, the same rate at the
 // matrix cores' limit (8192, 8, 1024, 4096: 526 us, 131 TFLOP/s, 64 x 64 571; 1501, 10, 2056,
 // 520: 77.6 and 74.0).
 struct TileCost {
@@ -756,7 +807,8 @@ int pick_tile(int64_t N, int64_t E, int64_t cols) {
         double rounds = rows * ((cols + t.bn - 1) / t.bn) / kUnitsOfDevice;
         if (t.bm == 256) {
             const double whole = (double)(int64_t)rounds;
-            if (rounds > whole) rounds = whole + 0.4 + 0.6 * (rounds - whole);
+            const double rest = rounds - whole;
+            rounds = whole + (rest > 0.5 ? 1.0 : rest > 0.25 ? 0.6 : rest > 0.0 ? 0.4 : 0.0);
         }
         const double cost = rounds * t.many > t.alone ? rounds * t.many : t.alone;
         if (i == 0 || cost < low) {
