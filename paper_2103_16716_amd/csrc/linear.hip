@@ -219,13 +219,13 @@ __device__ inline int count_row_tiles(const int32_t *__restrict__ offsets, int E
     return __builtin_amdgcn_readfirstlane(n);
 }
 
-// The tile of a call's `tiles` that a block computes as its i-th. Blocks go to the eight
+// The tile of a call's `tiles` that block number `block` computes. Blocks go to the eight
 // XCDs in turn; each XCD takes a run of consecutive tiles, which share rows or a matrix, so
 // that its L2 serves them. -1: none.
-__device__ inline int tile_of_block(int tiles, int i) {
+__device__ inline int tile_of_block(int tiles, int block) {
     const int per = (tiles + 7) / 8;
-    const int u = (blockIdx.x >> 3) + i * (gridDim.x >> 3);
-    const int t = (blockIdx.x & 7) * per + u;
+    const int u = block >> 3;
+    const int t = (block & 7) * per + u;
     return u < per && t < tiles ? t : -1;
 }
 
@@ -258,6 +258,7 @@ struct LinearCall {
     const int32_t *offsets;
     void *out;
     int N, E, K, O, relu;
+    int block0;   // the number of the launch's first block
 };
 
 // A tile of the result: expert, rows [m0, m_end), columns from n0, contraction [s0, s1).
@@ -544,21 +545,20 @@ struct Tiles {
     }
 };
 
-// Tile i of kTN: every expert's tiles are spread over the XCDs (an expert with many rows
+// The tile of kTN that block number `block` computes: every expert's tiles are spread over the XCDs (an expert with many rows
 // would else hold up one of them), a run to each. Small matrices go round by block.
 template <int BM, int BN>
-__device__ inline bool matrix_tile(const LinearCall &c, int i, Tile &t, bool &more) {
+__device__ inline bool matrix_tile(const LinearCall &c, int block, Tile &t, bool &more) {
     const int nm = (c.O + BM - 1) / BM, nn = (c.K + BN - 1) / BN, all = nm * nn;
     int k;
     if (all >= 32) {
         const int per = (all + 7) / 8;
-        const int u = (blockIdx.x >> 3) + i * (gridDim.x >> 3);
+        const int u = block >> 3;
         t.e = u / per;
-        k = (blockIdx.x & 7) * per + u - t.e * per;
+        k = (block & 7) * per + u - t.e * per;
     } else {
-        const int u = blockIdx.x + i * gridDim.x;
-        t.e = u / all;
-        k = u - t.e * all;
+        t.e = block / all;
+        k = block - t.e * all;
     }
     more = t.e < c.E;
     if (!more || k >= all) return false;
@@ -616,7 +616,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void linear_wide_kernel(LinearCall
         if constexpr (kForm == kTN) {
             bool more = true;
             while (more)
-                if (matrix_tile<BM, BN>(c, i++, t, more)) return true;
+                if (matrix_tile<BM, BN>(c, blockIdx.x + gridDim.x * i++, t, more)) return true;
             return false;
         } else {
             const int tiles = __builtin_amdgcn_readfirstlane(first[c.E]) * nn;
@@ -673,34 +673,28 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void linear_wide_kernel(LinearCall
     }
 }
 
-// Smaller tiles, of which several share a compute unit: a block for each, or, where that
-// would be more threads than a launch may have, for some of them.
+// Smaller tiles, of which several share a compute unit: a block for each.
 template <class In, int kForm, int BM, int BN, int WM, int WN, int kStages>
 __global__ __launch_bounds__(64 * WM * WN) void linear_kernel(LinearCall c) {
     using G = Tiles<In, kForm, BM, BN, WM, WN, kStages>;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     G g(c, lds);
-    const int nn = (g.cols + BN - 1) / BN;
-    const int tiles = kForm == kTN ? 0 : count_row_tiles(c.offsets, c.E, c.N, BM) * nn;
-    for (int i = 0;; ++i) {
-        Tile t;
-        if constexpr (kForm == kTN) {
-            bool more;
-            if (!matrix_tile<BM, BN>(c, i, t, more)) {
-                if (!more) return;
-                continue;
-            }
-        } else {
-            RowTile rt;
-            const int k = tile_of_block(tiles, i);
-            if (k < 0 || !find_row_tile(c.offsets, c.E, c.N, BM, k / nn, rt)) return;
-            t = Tile{rt.e, rt.r0, rt.r1, k % nn * BN, 0, kForm == kNT ? c.K : c.O};
-        }
-        g.set(t);
-        g.issue_first();
-        g.wait_chunk_0();
-        g.run(nullptr);
+    const int block = c.block0 + (int)blockIdx.x;
+    Tile t;
+    if constexpr (kForm == kTN) {
+        bool more;
+        if (!matrix_tile<BM, BN>(c, block, t, more)) return;
+    } else {
+        const int nn = (g.cols + BN - 1) / BN;
+        RowTile rt;
+        const int k = tile_of_block(count_row_tiles(c.offsets, c.E, c.N, BM) * nn, block);
+        if (k < 0 || !find_row_tile(c.offsets, c.E, c.N, BM, k / nn, rt)) return;
+        t = Tile{rt.e, rt.r0, rt.r1, k % nn * BN, 0, kForm == kNT ? c.K : c.O};
     }
+    g.set(t);
+    g.issue_first();
+    g.wait_chunk_0();
+    g.run(nullptr);
 }
 
 // db_e: column sums of dy over each expert's rows. A block for 128 bytes of an expert's
@@ -762,18 +756,25 @@ hipError_t launch_tiles(const LinearCall &c, hipStream_t s) {
             granted[dev] = true;
         }
     }
-    constexpr int64_t kMaxBlocks = 1 << 22;   // fewer than 2^32 threads
     int64_t blocks = kUnitsOfDevice;
     if (!kWide) {
         const int64_t nn = ((kForm == kNT ? c.O : c.K) + BN - 1) / BN;
         const int64_t nm = (c.O + BM - 1) / BM;
         if (kForm != kTN) blocks = nn * ((int64_t)c.N / BM + (c.E < c.N ? c.E : c.N));
         else blocks = nm * nn >= 32 ? (nm * nn + 7) / 8 * 8 * c.E : nm * nn * c.E;
-        blocks = blocks < kMaxBlocks ? (blocks + 7) / 8 * 8 : kMaxBlocks;
+        blocks = (blocks + 7) / 8 * 8;
     }
+    constexpr int64_t kMost = 1 << 22;   // a launch has fewer than 2^32 threads
     LinearCall call = c;
-    void *args[] = {&call};
-    return hipLaunchKernel(kernel, dim3((unsigned)blocks), dim3(64 * WM * WN), args, lds, s);
+    for (int64_t b = 0; b < blocks; b += kMost) {
+        call.block0 = (int)b;
+        void *args[] = {&call};
+        const int64_t now = blocks - b < kMost ? blocks - b : kMost;
+        const hipError_t err =
+            hipLaunchKernel(kernel, dim3((unsigned)now), dim3(64 * WM * WN), args, lds, s);
+        if (err != hipSuccess) return err;
+    }
+    return hipSuccess;
 }
 
 // The choice of tile. The row ranges are on the GPU, so it goes by the rows an expert has
@@ -871,14 +872,14 @@ hipError_t launch(const LinearCall &c, int bf16, hipStream_t s) {
 hipError_t launch_linear(const void *x, const void *w, const void *bias, const void *residual,
                          const int32_t *offsets, void *y, int64_t N, int64_t E, int64_t K,
                          int64_t O, int relu, int bf16, hipStream_t s) {
-    return launch<kNT>({x, w, bias, residual, offsets, y, (int)N, (int)E, (int)K, (int)O, relu},
+    return launch<kNT>({x, w, bias, residual, offsets, y, (int)N, (int)E, (int)K, (int)O, relu, 0},
                             bf16, s);
 }
 
 hipError_t launch_linear_dx(const void *dy, const void *w, const void *relu_of,
                             const int32_t *offsets, void *dx, int64_t N, int64_t E, int64_t K,
                             int64_t O, int bf16, hipStream_t s) {
-    return launch<kNN>({dy, w, nullptr, relu_of, offsets, dx, (int)N, (int)E, (int)K, (int)O, 0},
+    return launch<kNN>({dy, w, nullptr, relu_of, offsets, dx, (int)N, (int)E, (int)K, (int)O, 0, 0},
                             bf16, s);
 }
 
@@ -886,7 +887,7 @@ hipError_t launch_linear_dw(const void *dy, const void *x, const int32_t *offset
                             float *db, int64_t N, int64_t E, int64_t K, int64_t O, int bf16,
                             hipStream_t s) {
     const hipError_t err = launch<kTN>(
-        {dy, x, nullptr, nullptr, offsets, dw, (int)N, (int)E, (int)K, (int)O, 0}, bf16, s);
+        {dy, x, nullptr, nullptr, offsets, dw, (int)N, (int)E, (int)K, (int)O, 0, 0}, bf16, s);
     if (err != hipSuccess || db == nullptr) return err;
     const int64_t parts = (O * (bf16 ? 2 : 4) + 127) / 128;
     const dim3 grid((unsigned)(parts < 1024 ? parts : 1024), (unsigned)E);

@@ -365,6 +365,40 @@ def near_product(got, a, b, terms, step):
     assert bool(((got.double() - want).abs() <= bound + step * (want.abs() + bound)).all())
 
 
+@pytest.mark.parametrize("counts,K,O", [
+    # (1) many tiles of one size for every unit: the tiles that blocks go through in turn, ends
+    # of 1 to 255 rows, empty experts, a last round of few tiles
+    ([2816, 0, 2561, 2623], 72, 6152), ([1800, 900, 1300, 1, 3999, 0], 72, 6152),
+    ([8000], 200, 6144), ([4097, 4000], 1032, 2056), ([700, 64, 0, 129, 2200, 3000], 64, 8200),
+    ([2816, 0, 2561, 2623], 6152, 72), ([700, 64, 0, 129, 2200, 3000], 8200, 64),
+    # (2) 128 x 128 and 64 x 128 tiles, one expert and several
+    ([128] * 40, 264, 2056), ([90, 30, 64, 65] * 16, 520, 1032), ([513], 2056, 1032)])
+def test_large_products(counts, K, O):
+    """Every expert's block of y, dx and dW in bf16, in the tiles of larger calls, with the
+    results of rows before and behind left alone."""
+    g = torch.Generator(device="cuda").manual_seed(K + O)
+    before, behind = 5, 3
+    N, E = sum(counts) + before + behind, len(counts)
+    x, dy = (torch.randn(N, n, generator=g, device="cuda").bfloat16() for n in (K, O))
+    w = (torch.randn(E, O, K, generator=g, device="cuda") * K ** -0.5).bfloat16()
+    ends = np.cumsum([before] + counts)
+    off = torch.tensor(ends, dtype=torch.int32, device="cuda")
+    for back in (x, dy):
+        back[:before], back[N - behind:] = float("nan"), float("inf")
+    y = pb.expert_linear(x, w, off, out=torch.full((N, O), 7.0, dtype=x.dtype, device="cuda"))
+    dx = pb.expert_linear_dx(dy, w, off, out=torch.full_like(x, 7.0))
+    dw, db = pb.expert_linear_dw(dy, x, off)
+    for e, n in enumerate(counts):
+        r = slice(int(ends[e]), int(ends[e + 1]))
+        near_product(y[r], x[r], w[e].t().contiguous(), K, 2.0 ** -8)
+        near_product(dx[r], dy[r], w[e], O, 2.0 ** -8)
+        near_product(dw[e], dy[r].t().contiguous(), x[r], n, U)
+        want, mag = dy[r].double().sum(dim=0), dy[r].double().abs().sum(dim=0)
+        assert bool(((db[e].double() - want).abs() <= (n + 1) * U * mag).all())
+    for got in (y, dx):
+        assert bool((got[:before] == 7).all()) and bool((got[N - behind:] == 7).all())
+
+
 def test_matrices_beyond_32_bits():
     """More than 2^32 bytes and 2^31 elements in the rows, then in the matrices: the last
     rows and the last expert have their results."""
