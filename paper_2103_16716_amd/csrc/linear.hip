@@ -240,19 +240,6 @@ __device__ inline void tile_in_strip(int i, int nm, int nn, int &m, int &n) {
     m = s * kStrip + r - n * h;
 }
 
-template <class In>
-__device__ inline void load8(const void *p, int64_t i, float (&v)[8]) {
-    if constexpr (In::kBf16) {
-        const u32x4_t x = *reinterpret_cast<const u32x4_t *>(static_cast<const uint16_t *>(p) + i);
-        RowChunk<true>::widen(x, v);
-    } else {
-        const float4 *q = reinterpret_cast<const float4 *>(static_cast<const float *>(p) + i);
-        const float4 x = q[0], y = q[1];
-        v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
-        v[4] = y.x, v[5] = y.y, v[6] = y.z, v[7] = y.w;
-    }
-}
-
 struct LinearCall {
     const void *A, *B, *bias, *extra;   // extra: the residual (kNT) or relu_of (kNN)
     const int32_t *offsets;
@@ -365,15 +352,16 @@ struct Tiles {
         else wait_first<0>();
     }
 
-    // The products of the tile, whose first chunks have been issued and whose chunk 0 has
-    // landed for this wave. The last quarter of a chunk is multiplied behind the barrier that
-    // hands its stage over: its operands are in registers by then, and the next chunk's
-    // first ones are read beside it. Behind the last barrier all stages are free.
     // 256 x 256 tiles load into the stage handed over in two parts, A behind the barrier and B
     // a quarter of a chunk later (both at once: 32768 rows x 2048 to 8192, 32 experts 1010 us,
     // 975 so; smaller tiles are bound by the loads and issue them at once: 8192 rows by columns
     // of 64 experts, 4096 to 1024, 209 us in two parts, 164 at once).
     static constexpr bool kSplit = BM == 256 && kStages == 2;
+
+    // The products of the tile, whose first chunks have been issued and whose chunk 0 has
+    // landed for this wave. The last quarter of a chunk is multiplied behind the barrier that
+    // hands its stage over: its operands are in registers by then, and the next chunk's
+    // first ones are read beside it. Behind the last barrier all stages are free.
     template <int X>
     __device__ void contract(f32x16_t (&acc)[X][TN]) const {
 #pragma unroll
@@ -427,6 +415,60 @@ struct Tiles {
         }
     }
 
+    // What is added to the results or (relu_of) masks them: the bias of the wave's columns,
+    // loaded before the products, and `extra`, loaded behind them at once and ahead of the next
+    // tile's chunks, 16 bytes each (fp32: twice). Loaded where they are used, each would wait
+    // for those chunks (32768 rows x 2048 to 8192: with bias and ReLU 1060 us, 964 so; with
+    // bias and residual 1284, 1042).
+    static constexpr int kWords = In::kBf16 ? 1 : 2;
+    template <int X>
+    struct Added {
+        u32x4_t bias[kForm == kNT ? TN : 1][2][kWords];
+        u32x4_t extra[kForm == kTN ? 1 : X][TN][2][kWords];
+        __device__ void load_bias(const Tiles &g) {
+            if (kForm != kNT || g.c.bias == nullptr) return;
+            const elem_t *row = static_cast<const elem_t *>(g.c.bias) + (int64_t)g.t.e * g.c.O;
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int p = 0; p < 2; ++p) {
+                    const int n = g.t.n0 + 32 * (g.wn * TN + j) + 16 * p + 8 * (g.lane >> 5);
+#pragma unroll
+                    for (int h = 0; h < kWords; ++h)
+                        bias[kForm == kNT ? j : 0][p][h] = RowChunk<In::kBf16>::fetch(
+                            row + (n < g.cols ? n : 0), h);
+                }
+        }
+        __device__ void load_extra(const Tiles &g) {
+            if (kForm == kTN || g.c.extra == nullptr) return;
+            const int rows = g.t.m_end - g.t.m0;
+#pragma unroll
+            for (int x = 0; x < X; ++x) {
+                const int r = 32 * (g.wm + WM * x) + (g.lane & 31);
+                const elem_t *row = static_cast<const elem_t *>(g.c.extra) +
+                                    (int64_t)(g.t.m0 + (r < rows ? r : rows - 1)) * g.cols;
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+#pragma unroll
+                    for (int p = 0; p < 2; ++p) {
+                        const int n = g.t.n0 + 32 * (g.wn * TN + j) + 16 * p + 8 * (g.lane >> 5);
+#pragma unroll
+                        for (int h = 0; h < kWords; ++h)
+                            extra[kForm == kTN ? 0 : x][j][p][h] =
+                                RowChunk<In::kBf16>::fetch(row + (n < g.cols ? n : 0), h);
+                    }
+            }
+        }
+        __device__ static void widen(const u32x4_t (&w)[kWords], float (&v)[8]) {
+            if constexpr (In::kBf16) {
+                RowChunk<true>::widen(w[0], v);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i >> 2][i & 3]);
+            }
+        }
+    };
+
     // Stores of a wave per 32 x 32 results, 16 bytes a lane each.
     static constexpr int kStores = 16 * kOutSize / 16;
 
@@ -435,7 +477,7 @@ struct Tiles {
     // the half waves, so that a lane has eight neighbouring columns. Lanes outside the
     // result store to nowhere, so that every wave issues the same number of stores.
     template <int X>
-    __device__ void finish(const Tile &d, f32x16_t (&acc)[X][TN]) const {
+    __device__ void finish(const Tile &d, f32x16_t (&acc)[X][TN], const Added<X> &added) const {
         const int half = lane >> 5;
         char *out = static_cast<char *>(c.out) +
                     ((kForm == kTN ? (int64_t)d.e * c.O * c.K : 0) + (int64_t)d.m0 * cols) * kOutSize;
@@ -476,10 +518,9 @@ struct Tiles {
                         }
                         const int n = nj + 16 * p + 8 * half;
                         const bool in = row_in && n < cols;
-                        const int64_t at = (int64_t)(d.m0 + r) * cols + n;
                         if (kForm == kNT && c.bias != nullptr) {
                             float u[8];
-                            load8<In>(c.bias, (int64_t)d.e * c.O + (n < cols ? n : 0), u);
+                            Added<X>::widen(added.bias[kForm == kNT ? j : 0][p], u);
 #pragma unroll
                             for (int i = 0; i < 8; ++i) v[i] += u[i];
                         }
@@ -489,7 +530,7 @@ struct Tiles {
                         }
                         if (c.extra != nullptr) {
                             float u[8];
-                            load8<In>(c.extra, in ? at : (int64_t)d.m0 * cols, u);
+                            Added<X>::widen(added.extra[kForm == kTN ? 0 : x][j][p], u);
 #pragma unroll
                             for (int i = 0; i < 8; ++i) {
                                 if (kForm == kNT) v[i] += u[i];
@@ -521,14 +562,18 @@ struct Tiles {
     template <int X>
     __device__ void compute(const Tile *next) {
         f32x16_t acc[X][TN];
+        Added<X> added;
+        added.load_bias(*this);
         contract<X>(acc);
+        added.load_extra(*this);
+        asm volatile("" ::: "memory");
         const Tile done = t;
         if (next != nullptr) {
             set(*next);
             issue_first();
             asm volatile("" ::: "memory");
         }
-        finish<X>(done, acc);
+        finish<X>(done, acc, added);
         if (next != nullptr) {
             asm volatile("" ::: "memory");
             constexpr int kBehind = X * TN * kStores;
