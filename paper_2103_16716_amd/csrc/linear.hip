@@ -229,15 +229,20 @@ __device__ inline int tile_of_block(int tiles, int block) {
     return u < per && t < tiles ? t : -1;
 }
 
-// Tile i of an expert's nm x nn, in strips of kStrip tiles of rows: neighbours in a strip
-// share columns, and the strip's rows stay in the L2 while its columns go by.
-constexpr int kStrip = 4;
+// Tile i of an expert's nm x nn, in strips of up to kMost tiles of rows, as equal as can be:
+// neighbours in a strip share columns, and the strip's rows stay in the L2 while its columns
+// go by. Eight for rows (32768 uneven rows x 2048 to 8192: 1034 us, 1051 with four; by columns
+// of 16384, 2048 to 8192, 575 and 590), four for the matrices' gradient (749 us, 802 with
+// eight).
+template <int kMost>
 __device__ inline void tile_in_strip(int i, int nm, int nn, int &m, int &n) {
-    const int s = i / (kStrip * nn);
-    const int r = i - s * kStrip * nn;
-    const int h = nm - s * kStrip < kStrip ? nm - s * kStrip : kStrip;
+    const int strips = (nm + kMost - 1) / kMost;
+    const int height = (nm + strips - 1) / strips;
+    const int s = i / (height * nn);
+    const int r = i - s * height * nn;
+    const int h = nm - s * height < height ? nm - s * height : height;
     n = r / h;
-    m = s * kStrip + r - n * h;
+    m = s * height + r - n * h;
 }
 
 struct LinearCall {
@@ -608,7 +613,7 @@ __device__ inline bool matrix_tile(const LinearCall &c, int block, Tile &t, bool
     more = t.e < c.E;
     if (!more || k >= all) return false;
     int m, n;
-    tile_in_strip(k, nm, nn, m, n);
+    tile_in_strip<4>(k, nm, nn, m, n);
     t.m0 = m * BM;
     t.m_end = c.O;
     t.n0 = n * BN;
@@ -694,7 +699,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void linear_wide_kernel(LinearCall
                 t.m_end = row_bound(c.offsets, e + 1, c.N);
                 int m, n;
                 const int nm = __builtin_amdgcn_readfirstlane(first[e + 1]) - f;
-                tile_in_strip(k - f * nn, nm, nn, m, n);
+                tile_in_strip<8>(k - f * nn, nm, nn, m, n);
                 t.m0 = a + m * BM + part * rows;
                 if (t.m0 >= t.m_end) continue;
                 if (t.m_end - t.m0 > rows) t.m_end = t.m0 + rows;
