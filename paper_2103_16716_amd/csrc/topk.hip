@@ -400,9 +400,12 @@ __global__ __launch_bounds__(64 * kWaves) void pair_place_kernel(
 }
 
 // Few tokens: the latency of launches is what counts, so one block does it all and keeps the
-// pairs' experts in LDS.
+// pairs' experts in LDS. us in a graph, one block and two launches: 64 tokens, 2 of 64 experts
+// 4.5 and 10; 256 tokens 7.6 and 10.1; 128 tokens, 8 of 256 13.0 and 15; 256 tokens 23.2 and
+// 15.5, so by the scores as well.
 constexpr int kSmallTokens = 256;
 constexpr int kSmallPairs = 2048;
+constexpr int kSmallScores = 32768;
 
 template <int G, int C, int L>
 __global__ __launch_bounds__(kThreads) void route_small_kernel(
@@ -432,7 +435,7 @@ struct RouteCall {
 };
 
 bool is_small(int64_t T, int64_t E, int64_t k) {
-    return T <= kSmallTokens && T * k <= kSmallPairs && E <= kScanFrom;
+    return T <= kSmallTokens && T * k <= kSmallPairs && T * E <= kSmallScores && E <= kScanFrom;
 }
 
 template <int G, int C, int L>

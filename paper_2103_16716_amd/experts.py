@@ -43,6 +43,20 @@ class Routing:
 def _need(**tensors) -> None:
     """Every given tensor contiguous and on the current device."""
     here = -1
+    for t in tensors.values():
+        if t is None:
+            continue
+        d = t.get_device()
+        if d != here or d < 0:
+            if here < 0 <= d:
+                here = _torch().cuda.current_device()
+            if d != here or d < 0:
+                _refuse(tensors, here)
+        if not t.is_contiguous():
+            _refuse(tensors, here)
+
+
+def _refuse(tensors, here) -> None:
     for name, t in tensors.items():
         if t is None:
             continue
@@ -51,10 +65,11 @@ def _need(**tensors) -> None:
         if not t.is_contiguous():
             raise ValueError(f"{name} must be contiguous")
         if t.get_device() != here:
-            if here < 0:
-                here = _torch().cuda.current_device()
-            if t.get_device() != here:
-                raise ValueError(f"{name} is on {t.device}, the current device is cuda:{here}")
+            raise ValueError(f"{name} is on {t.device}, the current device is cuda:{here}")
+
+
+def _empty(rows, cols, dtype, device):
+    return _torch().empty_strided((rows, cols), (cols, 1), dtype=dtype, device=device)
 
 
 def _like(name, t, shape, dtype) -> None:
@@ -132,7 +147,7 @@ def topk_assign(S, k: int, workspace=None, stream=None, out_assign=None, out_sco
         _like("out_scores", out_scores, (T, k), torch.float32)
         scores = out_scores
         if scores is None:
-            scores = torch.empty((T, k), dtype=torch.float32, device=dev)
+            scores = _empty(T, k, torch.float32, dev)
         ws = workspace
         if ws is None:
             ws = _workspace(topk_workspace_size(T, E, k), dev)
@@ -191,7 +206,7 @@ def dispatch(x, slots, weights=None, out=None, stream=None):
     _like("out", out, (T * k, d), x.dtype)
     with _on(stream):
         if out is None:
-            out = torch.empty((T * k, d), dtype=x.dtype, device=x.device)
+            out = _empty(T * k, d, x.dtype, x.device)
         _check(lib().base_dispatch(x.data_ptr(), _ptr(weights), slots.data_ptr(), out.data_ptr(),
                                    T, k, d, _dtype_code(x), _stream_ptr(stream)), "base_dispatch")
     return out
@@ -209,7 +224,7 @@ def combine(F, slots, weights=None, residual=None, out=None, stream=None):
     _like("out", out, (T, d), F.dtype)
     with _on(stream):
         if out is None:
-            out = torch.empty((T, d), dtype=F.dtype, device=F.device)
+            out = _empty(T, d, F.dtype, F.device)
         _check(lib().base_combine(F.data_ptr(), _ptr(weights), slots.data_ptr(), _ptr(residual),
                                   out.data_ptr(), T, k, d, _dtype_code(F), _stream_ptr(stream)),
                "base_combine")
@@ -231,7 +246,7 @@ def combine_backward(dY, F, slots, weights, out=None, stream=None):
     with _on(stream):
         if out is None:
             out = torch.empty_like(F)
-        dw = torch.empty((T, k), dtype=torch.float32, device=F.device)
+        dw = _empty(T, k, torch.float32, F.device)
         _check(lib().base_combine_backward(dY.data_ptr(), F.data_ptr(), weights.data_ptr(),
                                            slots.data_ptr(), out.data_ptr(), dw.data_ptr(), T, k,
                                            d, _dtype_code(F), _stream_ptr(stream)),
@@ -272,7 +287,7 @@ def expert_norm(x, weight, bias=None, offsets=None, eps: float = 1e-5, perm=None
     _like("out", out, (N, d), x.dtype)
     with _on(stream):
         if out is None:
-            out = torch.empty((N, d), dtype=x.dtype, device=x.device)
+            out = _empty(N, d, x.dtype, x.device)
         mean = torch.empty(N, dtype=torch.float32, device=x.device)
         rstd = torch.empty(N, dtype=torch.float32, device=x.device)
         _check(lib().base_expert_norm(x.data_ptr(), _ptr(perm), x.shape[0], k, weight.data_ptr(),
@@ -300,7 +315,7 @@ def expert_norm_backward(dy, x, weight, mean, rstd, offsets=None, perm=None, k: 
     _like("out", out, (N, d), x.dtype)
     with _on(stream):
         if out is None:
-            out = torch.empty((N, d), dtype=x.dtype, device=x.device)
+            out = _empty(N, d, x.dtype, x.device)
         dweight = torch.empty(weight.shape, dtype=torch.float32, device=x.device)
         dbias = torch.empty(weight.shape, dtype=torch.float32, device=x.device)
         ws = workspace
@@ -337,7 +352,7 @@ def expert_linear(x, w, offsets, bias=None, relu: bool = False, residual=None, o
     _like("out", out, (N, O), w.dtype)
     with _on(stream):
         if out is None:
-            out = torch.empty((N, O), dtype=x.dtype, device=x.device)
+            out = _empty(N, O, x.dtype, x.device)
         _check(lib().base_expert_linear(x.data_ptr(), w.data_ptr(), _ptr(bias), _ptr(residual),
                                         offsets.data_ptr(), out.data_ptr(), N, E, K, O,
                                         1 if relu else 0, _dtype_code(x), _stream_ptr(stream)),
@@ -357,7 +372,7 @@ def expert_linear_dx(dy, w, offsets, relu_of=None, out=None, stream=None):
     _like("out", out, (N, K), w.dtype)
     with _on(stream):
         if out is None:
-            out = torch.empty((N, K), dtype=dy.dtype, device=dy.device)
+            out = _empty(N, K, dy.dtype, dy.device)
         _check(lib().base_expert_linear_dx(dy.data_ptr(), w.data_ptr(), _ptr(relu_of),
                                            offsets.data_ptr(), out.data_ptr(), N, E, K, O,
                                            _dtype_code(dy), _stream_ptr(stream)),
@@ -378,7 +393,7 @@ def expert_linear_dw(dy, x, offsets, stream=None):
     _like("offsets", offsets, (E + 1,), torch.int32)
     with _on(stream):
         dw = torch.empty((E, O, K), dtype=torch.float32, device=dy.device)
-        db = torch.empty((E, O), dtype=torch.float32, device=dy.device)
+        db = _empty(E, O, torch.float32, dy.device)
         _check(lib().base_expert_linear_dw(dy.data_ptr(), x.data_ptr(), offsets.data_ptr(),
                                            dw.data_ptr(), db.data_ptr(), N, E, K, O,
                                            _dtype_code(dy), _stream_ptr(stream)),
