@@ -573,20 +573,29 @@ int base_expert_norm_backward(const void *dy, const void *x, const int32_t *perm
  *      left as they are.
  *   N < 2^31, E <= 2048, K % 8 == 0, O % 8 == 0, K, O <= 2^20; 16-byte aligned. y
  *   may be residual and dx may be relu_of; outputs overlap no other input.
+ *   workspace [device] base_expert_linear_workspace_size(product, N, E, K, O, dtype)
+ *      bytes, 256-aligned; any contents at entry. 0 (then workspace may be NULL) but for
+ *      calls with few outputs and a long sum, which is cut into parts.
  * Products are summed in fp32 (bf16 products are exact there; fp32 ones are not
  * reduced), in an order that depends on the sizes only: the same call gives the
  * same bits every time.
- * Errors: BASE_ERR_INVALID_ARG, BASE_ERR_UNSUPPORTED_DTYPE, BASE_ERR_RANGE, BASE_ERR_HIP.
+ * Errors: BASE_ERR_INVALID_ARG, BASE_ERR_UNSUPPORTED_DTYPE, BASE_ERR_RANGE,
+ * BASE_ERR_WORKSPACE, BASE_ERR_HIP.
  */
+typedef enum { BASE_PRODUCT_Y = 0, BASE_PRODUCT_DX = 1, BASE_PRODUCT_DW = 2 } base_product;
+
+size_t base_expert_linear_workspace_size(int product, int64_t N, int64_t E, int64_t K, int64_t O,
+                                         int dtype);
 int base_expert_linear(const void *x, const void *w, const void *bias, const void *residual,
                        const int32_t *offsets, void *y, int64_t N, int64_t E, int64_t K, int64_t O,
-                       int relu, int dtype, void *stream);
+                       int relu, int dtype, void *workspace, size_t workspace_bytes, void *stream);
 int base_expert_linear_dx(const void *dy, const void *w, const void *relu_of,
                           const int32_t *offsets, void *dx, int64_t N, int64_t E, int64_t K,
-                          int64_t O, int dtype, void *stream);
+                          int64_t O, int dtype, void *workspace, size_t workspace_bytes,
+                          void *stream);
 int base_expert_linear_dw(const void *dy, const void *x, const int32_t *offsets, float *dw,
                           float *db, int64_t N, int64_t E, int64_t K, int64_t O, int dtype,
-                          void *stream);
+                          void *workspace, size_t workspace_bytes, void *stream);
 
 /* ------------------------------------------------------------------------ */
 /* Measurement support                                                       */

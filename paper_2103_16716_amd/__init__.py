@@ -36,6 +36,10 @@ BASE_F32 = 0
 BASE_BF16 = 1
 BASE_I16 = 2
 
+BASE_PRODUCT_Y = 0
+BASE_PRODUCT_DX = 1
+BASE_PRODUCT_DW = 2
+
 BASE_ASSIGN_GREEDY_FALLBACK = 1
 BASE_ASSIGN_SYNC_STATS = 2
 BASE_ASSIGN_CHECK_FINITE = 4
@@ -51,7 +55,8 @@ EXPORTED = ("base_status_string", "base_affinity", "base_affinity_gather",
             "base_timing_read", "base_topk_workspace_size", "base_topk_assign",
             "base_sort_by_expert", "base_dispatch", "base_combine", "base_combine_backward",
             "base_expert_norm", "base_expert_norm_workspace_size", "base_expert_norm_backward",
-            "base_expert_linear", "base_expert_linear_dx", "base_expert_linear_dw")
+            "base_expert_linear_workspace_size", "base_expert_linear", "base_expert_linear_dx",
+            "base_expert_linear_dw")
 
 
 class AssignOpts(ctypes.Structure):
@@ -136,14 +141,18 @@ def lib() -> ctypes.CDLL:
                                 ctypes.c_double, i32, vp],
                 "expert_norm_backward": [vp, vp, vp, i64, i64, vp, vp, vp, vp, vp, vp, vp, vp,
                                          i64, i64, i64, i32, vp, sz, vp],
-                "expert_linear": [vp, vp, vp, vp, vp, vp, i64, i64, i64, i64, i32, i32, vp],
-                "expert_linear_dx": [vp, vp, vp, vp, vp, i64, i64, i64, i64, i32, vp],
-                "expert_linear_dw": [vp, vp, vp, vp, vp, i64, i64, i64, i64, i32, vp]}.items():
+                "expert_linear": [vp, vp, vp, vp, vp, vp, i64, i64, i64, i64, i32, i32, vp, sz,
+                                  vp],
+                "expert_linear_dx": [vp, vp, vp, vp, vp, i64, i64, i64, i64, i32, vp, sz, vp],
+                "expert_linear_dw": [vp, vp, vp, vp, vp, i64, i64, i64, i64, i32, vp, sz,
+                                     vp]}.items():
             fn = getattr(L, "base_" + name)
             fn.argtypes, fn.restype = args, i32
         for name in ("topk_workspace_size", "expert_norm_workspace_size"):
             fn = getattr(L, "base_" + name)
             fn.argtypes, fn.restype = [i64, i64, i64], sz
+        L.base_expert_linear_workspace_size.argtypes = [i32, i64, i64, i64, i64, i32]
+        L.base_expert_linear_workspace_size.restype = sz
         L.base_timing_enable.argtypes = [ctypes.c_int32]
         L.base_timing_enable.restype = i32
         L.base_timing_read.argtypes = [ctypes.POINTER(i64), ctypes.POINTER(ctypes.c_double)]
@@ -508,8 +517,8 @@ def timing_read() -> tuple[int, float]:
 
 
 from .experts import (Routing, combine, combine_backward, dispatch, expert_linear,  # noqa: E402
-                      expert_linear_dw, expert_linear_dx, expert_norm, expert_norm_backward,
-                      expert_norm_workspace_size, sort_by_expert, topk_assign,
+                      expert_linear_dw, expert_linear_dx, expert_linear_workspace_size, expert_norm,
+                      expert_norm_backward, expert_norm_workspace_size, sort_by_expert, topk_assign,
                       topk_workspace_size)
 
 __all__ = ["affinity", "assign", "assign_batched", "permute", "permute_batched", "greedy_assign",
@@ -521,4 +530,4 @@ __all__ = ["affinity", "assign", "assign_batched", "permute", "permute_batched",
            "status_string", "EXPORTED", "Routing", "topk_assign", "topk_workspace_size",
            "sort_by_expert", "dispatch", "combine", "combine_backward", "expert_norm",
            "expert_norm_workspace_size", "expert_norm_backward", "expert_linear",
-           "expert_linear_dx", "expert_linear_dw"]
+           "expert_linear_dx", "expert_linear_dw", "expert_linear_workspace_size"]

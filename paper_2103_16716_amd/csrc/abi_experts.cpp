@@ -69,6 +69,12 @@ int check_linear(int64_t N, int64_t E, int64_t K, int64_t O, int dtype) {
     return BASE_OK;
 }
 
+bool has_workspace(int product, int64_t N, int64_t E, int64_t K, int64_t O, int dtype,
+                   const void *workspace, size_t bytes) {
+    const size_t need = base::linear_workspace_size(product, N, E, K, O, dtype == BASE_BF16);
+    return need == 0 || (workspace != nullptr && bytes >= need && aligned(workspace, 256));
+}
+
 }  // namespace
 
 extern "C" {
@@ -209,9 +215,17 @@ int base_expert_norm_backward(const void *dy, const void *x, const int32_t *perm
                                                  static_cast<hipStream_t>(stream)));
 }
 
+size_t base_expert_linear_workspace_size(int product, int64_t N, int64_t E, int64_t K, int64_t O,
+                                         int dtype) {
+    if (product < BASE_PRODUCT_Y || product > BASE_PRODUCT_DW) return 0;
+    if (check_linear(N, E, K, O, dtype) != BASE_OK) return 0;
+    return base::linear_workspace_size(product, N, E, K, O, dtype == BASE_BF16);
+}
+
 int base_expert_linear(const void *x, const void *w, const void *bias, const void *residual,
                        const int32_t *offsets, void *y, int64_t N, int64_t E, int64_t K, int64_t O,
-                       int relu, int dtype, void *stream) {
+                       int relu, int dtype, void *workspace, size_t workspace_bytes,
+                       void *stream) {
     if (x == nullptr || w == nullptr || offsets == nullptr || y == nullptr)
         return BASE_ERR_INVALID_ARG;
     if (const int st = check_linear(N, E, K, O, dtype)) return st;
@@ -223,13 +237,17 @@ int base_expert_linear(const void *x, const void *w, const void *bias, const voi
     if (overlap(y, N * O * sz, x, N * K * sz) || overlap(y, N * O * sz, w, E * O * K * sz) ||
         partly(y, residual, N * O * sz))
         return BASE_ERR_INVALID_ARG;
+    if (!has_workspace(BASE_PRODUCT_Y, N, E, K, O, dtype, workspace, workspace_bytes))
+        return BASE_ERR_WORKSPACE;
     return hip_status(base::launch_linear(x, w, bias, residual, offsets, y, N, E, K, O, relu,
-                                          dtype == BASE_BF16, static_cast<hipStream_t>(stream)));
+                                          dtype == BASE_BF16, workspace,
+                                          static_cast<hipStream_t>(stream)));
 }
 
 int base_expert_linear_dx(const void *dy, const void *w, const void *relu_of,
                           const int32_t *offsets, void *dx, int64_t N, int64_t E, int64_t K,
-                          int64_t O, int dtype, void *stream) {
+                          int64_t O, int dtype, void *workspace, size_t workspace_bytes,
+                          void *stream) {
     if (dy == nullptr || w == nullptr || offsets == nullptr || dx == nullptr)
         return BASE_ERR_INVALID_ARG;
     if (const int st = check_linear(N, E, K, O, dtype)) return st;
@@ -240,14 +258,16 @@ int base_expert_linear_dx(const void *dy, const void *w, const void *relu_of,
     if (overlap(dx, N * K * sz, dy, N * O * sz) || overlap(dx, N * K * sz, w, E * O * K * sz) ||
         partly(dx, relu_of, N * K * sz))
         return BASE_ERR_INVALID_ARG;
+    if (!has_workspace(BASE_PRODUCT_DX, N, E, K, O, dtype, workspace, workspace_bytes))
+        return BASE_ERR_WORKSPACE;
     return hip_status(base::launch_linear_dx(dy, w, relu_of, offsets, dx, N, E, K, O,
-                                             dtype == BASE_BF16,
+                                             dtype == BASE_BF16, workspace,
                                              static_cast<hipStream_t>(stream)));
 }
 
 int base_expert_linear_dw(const void *dy, const void *x, const int32_t *offsets, float *dw,
                           float *db, int64_t N, int64_t E, int64_t K, int64_t O, int dtype,
-                          void *stream) {
+                          void *workspace, size_t workspace_bytes, void *stream) {
     if (dy == nullptr || x == nullptr || offsets == nullptr || dw == nullptr)
         return BASE_ERR_INVALID_ARG;
     if (const int st = check_linear(N, E, K, O, dtype)) return st;
@@ -258,8 +278,10 @@ int base_expert_linear_dw(const void *dy, const void *x, const int32_t *offsets,
     if (overlap(dw, E * O * K * 4, dy, N * O * sz) || overlap(dw, E * O * K * 4, x, N * K * sz) ||
         overlap(dw, E * O * K * 4, db, E * O * 4))
         return BASE_ERR_INVALID_ARG;
+    if (!has_workspace(BASE_PRODUCT_DW, N, E, K, O, dtype, workspace, workspace_bytes))
+        return BASE_ERR_WORKSPACE;
     return hip_status(base::launch_linear_dw(dy, x, offsets, dw, db, N, E, K, O,
-                                             dtype == BASE_BF16,
+                                             dtype == BASE_BF16, workspace,
                                              static_cast<hipStream_t>(stream)));
 }
 

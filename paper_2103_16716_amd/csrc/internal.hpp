@@ -137,16 +137,18 @@ hipError_t launch_norm_backward(const void *dy, const void *x, const int32_t *pe
                                 void *dx, float *dweight, float *dbias, int64_t N, int64_t E,
                                 int64_t d, int bf16, void *workspace, hipStream_t s);
 
-// The experts' products over N routed rows, w [E, O, K] (linear.hip).
+// The experts' products over N routed rows, w [E, O, K] (linear.hip); product: a
+// base_product.
+size_t linear_workspace_size(int product, int64_t N, int64_t E, int64_t K, int64_t O, int bf16);
 hipError_t launch_linear(const void *x, const void *w, const void *bias, const void *residual,
                          const int32_t *offsets, void *y, int64_t N, int64_t E, int64_t K,
-                         int64_t O, int relu, int bf16, hipStream_t s);
+                         int64_t O, int relu, int bf16, void *workspace, hipStream_t s);
 hipError_t launch_linear_dx(const void *dy, const void *w, const void *relu_of,
                             const int32_t *offsets, void *dx, int64_t N, int64_t E, int64_t K,
-                            int64_t O, int bf16, hipStream_t s);
+                            int64_t O, int bf16, void *workspace, hipStream_t s);
 hipError_t launch_linear_dw(const void *dy, const void *x, const int32_t *offsets, float *dw,
                             float *db, int64_t N, int64_t E, int64_t K, int64_t O, int bf16,
-                            hipStream_t s);
+                            void *workspace, hipStream_t s);
 
 // Event timing of the engine kernel's launches (measurement support).
 hipError_t timing_enable(int32_t capacity);

@@ -65,7 +65,7 @@ __device__ inline bool find_row_tile(const int32_t *__restrict__ offsets, int E,
 }
 
 
-enum { kNT, kNN, kTN };
+enum { kNT = BASE_PRODUCT_Y, kNN = BASE_PRODUCT_DX, kTN = BASE_PRODUCT_DW };
 
 // 16 bytes of an operand's contraction per lane. bf16: one instruction multiplies the
 // lanes' 8 elements; fp32: four, instruction i the lanes' element i.
@@ -251,6 +251,10 @@ struct LinearCall {
     void *out;
     int N, E, K, O, relu;
     int block0;   // the number of the launch's first block
+    // The contraction in `parts`, part p by blocks [p per_part, (p + 1) per_part), whose results
+    // follow each other in `out`, part_size of them (fp32) each.
+    int parts, per_part;
+    int64_t part_size;
 };
 
 // A tile of the result: expert, rows [m0, m_end), columns from n0, contraction [s0, s1).
@@ -262,7 +266,7 @@ struct Tile {
 // 32 rows and TN x 32 neighbouring columns, so that a tile with few rows left (the end of an
 // expert) is spread over the waves, which skip what lies behind: the loop is compiled for
 // each number of 32 rows a wave may have.
-template <class In, int kForm, int BM, int BN, int WM, int WN, int kStages>
+template <class In, int kForm, int BM, int BN, int WM, int WN, int kStages, bool kPartial = false>
 struct Tiles {
     using unit_t = typename In::unit_t;
     using elem_t = typename In::elem_t;
@@ -274,7 +278,8 @@ struct Tiles {
     static constexpr int64_t kSize = sizeof(elem_t);
     static constexpr int kBytes = StageA::kBytes + StageB::kBytes;
     static constexpr int kLoads = StageA::kSlots + StageB::kSlots;   // of a wave, per stage
-    static constexpr int kOutSize = kForm == kTN ? 4 : (int)kSize;
+    static constexpr bool kSums = kForm == kTN || kPartial;   // results stored as fp32 sums
+    static constexpr int kOutSize = kSums ? 4 : (int)kSize;
 
     const LinearCall &c;
     char *lds;
@@ -312,8 +317,8 @@ struct Tiles {
         A = static_cast<const char *>(c.A);
         B = static_cast<const char *>(c.B);
         if (kForm != kTN) B += (int64_t)t.e * c.O * ldb;
-        A += kForm == kTN ? t.s0 * lda + t.m0 * kSize : t.m0 * lda;
-        B += kForm == kTN ? t.s0 * ldb + t.n0 * kSize : kForm == kNN ? t.n0 * kSize : t.n0 * ldb;
+        A += kForm == kTN ? t.s0 * lda + t.m0 * kSize : t.m0 * lda + t.s0 * kSize;
+        B += kForm == kNT ? t.n0 * ldb + t.s0 * kSize : t.s0 * ldb + t.n0 * kSize;
         nk = t.s1 > t.s0 ? (t.s1 - t.s0 - 1) / S + 1 : 0;
     }
     // The loads of chunk kc into stage st, of operand A (1), B (2) or both.
@@ -324,8 +329,9 @@ struct Tiles {
         const int rows = t.m_end - t.m0 < BM ? t.m_end - t.m0 : BM;
         const int64_t step_a = kForm == kTN ? S * lda : kChunk;
         const int64_t step_b = kForm == kNT ? kChunk : S * ldb;
-        const int64_t end_a = kForm == kTN ? steps * lda - t.m0 * kSize : rows * lda - kc * kChunk;
-        const int64_t end_b = kForm == kNT ? ncols * ldb - kc * kChunk : steps * ldb - t.n0 * kSize;
+        const int64_t before = t.s0 * kSize + kc * kChunk;   // of a row, along the contraction
+        const int64_t end_a = kForm == kTN ? steps * lda - t.m0 * kSize : rows * lda - before;
+        const int64_t end_b = kForm == kNT ? ncols * ldb - before : steps * ldb - t.n0 * kSize;
         if (which & 1) sa.load(A + kc * step_a, (uint32_t)end_a, left, base);
         if (which & 2) sb.load(B + kc * step_b, (uint32_t)end_b, left, base + StageA::kBytes);
     }
@@ -429,9 +435,9 @@ struct Tiles {
     template <int X>
     struct Added {
         u32x4_t bias[kForm == kNT ? TN : 1][2][kWords];
-        u32x4_t extra[kForm == kTN ? 1 : X][TN][2][kWords];
+        u32x4_t extra[kSums ? 1 : X][TN][2][kWords];
         __device__ void load_bias(const Tiles &g) {
-            if (kForm != kNT || g.c.bias == nullptr) return;
+            if (kSums || kForm != kNT || g.c.bias == nullptr) return;
             const elem_t *row = static_cast<const elem_t *>(g.c.bias) + (int64_t)g.t.e * g.c.O;
 #pragma unroll
             for (int j = 0; j < TN; ++j)
@@ -445,7 +451,7 @@ struct Tiles {
                 }
         }
         __device__ void load_extra(const Tiles &g) {
-            if (kForm == kTN || g.c.extra == nullptr) return;
+            if (kSums || g.c.extra == nullptr) return;
             const int rows = g.t.m_end - g.t.m0;
 #pragma unroll
             for (int x = 0; x < X; ++x) {
@@ -459,7 +465,7 @@ struct Tiles {
                         const int n = g.t.n0 + 32 * (g.wn * TN + j) + 16 * p + 8 * (g.lane >> 5);
 #pragma unroll
                         for (int h = 0; h < kWords; ++h)
-                            extra[kForm == kTN ? 0 : x][j][p][h] =
+                            extra[kSums ? 0 : x][j][p][h] =
                                 RowChunk<In::kBf16>::fetch(row + (n < g.cols ? n : 0), h);
                     }
             }
@@ -495,7 +501,7 @@ struct Tiles {
 #pragma unroll
             for (int j = 0; j < TN; ++j) {
                 const int nj = d.n0 + 32 * (wn * TN + j);
-                if constexpr (kForm == kTN) {
+                if constexpr (kSums) {
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
                         const int n = nj + 8 * q + 4 * half;
@@ -535,7 +541,7 @@ struct Tiles {
                         }
                         if (c.extra != nullptr) {
                             float u[8];
-                            Added<X>::widen(added.extra[kForm == kTN ? 0 : x][j][p], u);
+                            Added<X>::widen(added.extra[kSums ? 0 : x][j][p], u);
 #pragma unroll
                             for (int i = 0; i < 8; ++i) {
                                 if (kForm == kNT) v[i] += u[i];
@@ -723,13 +729,20 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void linear_wide_kernel(LinearCall
     }
 }
 
-// Smaller tiles, of which several share a compute unit: a block for each.
-template <class In, int kForm, int BM, int BN, int WM, int WN, int kStages>
+// Smaller tiles, of which several share a compute unit: a block for each. kPartial: for each
+// part of the contraction.
+template <class In, int kForm, int BM, int BN, int WM, int WN, int kStages, bool kPartial>
 __global__ __launch_bounds__(64 * WM * WN) void linear_kernel(LinearCall c) {
-    using G = Tiles<In, kForm, BM, BN, WM, WN, kStages>;
+    using G = Tiles<In, kForm, BM, BN, WM, WN, kStages, kPartial>;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
+    int block = c.block0 + (int)blockIdx.x;
+    int part = 0;
+    if constexpr (kPartial) {
+        part = block / c.per_part;
+        block -= part * c.per_part;
+        c.out = static_cast<float *>(c.out) + part * c.part_size;
+    }
     G g(c, lds);
-    const int block = c.block0 + (int)blockIdx.x;
     Tile t;
     if constexpr (kForm == kTN) {
         bool more;
@@ -741,24 +754,109 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_kernel(LinearCall c) {
         if (k < 0 || !find_row_tile(c.offsets, c.E, c.N, BM, k / nn, rt)) return;
         t = Tile{rt.e, rt.r0, rt.r1, k % nn * BN, 0, kForm == kNT ? c.K : c.O};
     }
+    if constexpr (kPartial) {   // whole chunks; the last parts may have none
+        const int chunks = t.s1 > t.s0 ? (t.s1 - t.s0 - 1) / G::S + 1 : 0;
+        const int per = (chunks + c.parts - 1) / c.parts;
+        const int first = part * per < chunks ? part * per : chunks;
+        const int last = first + per < chunks ? first + per : chunks;
+        if (last < chunks) t.s1 = t.s0 + last * G::S;
+        t.s0 = first < chunks ? t.s0 + first * G::S : t.s1;
+    }
     g.set(t);
     g.issue_first();
     g.wait_chunk_0();
     g.run(nullptr);
 }
 
+// The parts' sums of y or dx, added up in their order, and what follows the product. A wave
+// for 512 columns of a row.
+template <class In, int kForm>
+__global__ __launch_bounds__(256) void join_rows_kernel(LinearCall c, const float *part) {
+    using Ck = RowChunk<In::kBf16>;
+    constexpr int kSteps = 8 / Ck::kN;
+    const int cols = kForm == kNT ? c.O : c.K;
+    const int groups = (cols + 511) / 512;
+    const int lane = threadIdx.x & 63;
+    for (int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); w < (int64_t)c.N * groups;
+         w += (int64_t)gridDim.x * 4) {
+        const int r = (int)(w / groups);
+        const int n = (int)(w % groups) * 512 + 8 * lane;
+        if (r < c.offsets[0]) continue;
+        const int e = expert_of_row(c.offsets, c.E, r);
+        if (e >= c.E || n >= cols) continue;
+        const int64_t at = (int64_t)r * cols + n;
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = 0.0f;
+#pragma unroll 8
+        for (int p = 0; p < c.parts; ++p) {
+            const float4 *q = reinterpret_cast<const float4 *>(part + p * c.part_size + at);
+            const float4 x = q[0], y = q[1];
+            v[0] += x.x, v[1] += x.y, v[2] += x.z, v[3] += x.w;
+            v[4] += y.x, v[5] += y.y, v[6] += y.z, v[7] += y.w;
+        }
+#pragma unroll
+        for (int h = 0; h < kSteps; ++h) {
+            float u[Ck::kN], o[Ck::kN];
+#pragma unroll
+            for (int i = 0; i < Ck::kN; ++i) o[i] = v[h * Ck::kN + i];
+            const int64_t chunk = at / Ck::kN + h;
+            if (kForm == kNT && c.bias != nullptr) {
+                Ck::widen(Ck::fetch(c.bias, ((int64_t)e * c.O + n) / Ck::kN + h), u);
+#pragma unroll
+                for (int i = 0; i < Ck::kN; ++i) o[i] += u[i];
+            }
+            if (kForm == kNT && c.relu) {
+#pragma unroll
+                for (int i = 0; i < Ck::kN; ++i) o[i] = o[i] < 0.0f ? 0.0f : o[i];
+            }
+            if (c.extra != nullptr) {
+                Ck::widen(Ck::fetch(c.extra, chunk), u);
+#pragma unroll
+                for (int i = 0; i < Ck::kN; ++i) {
+                    if (kForm == kNT) o[i] += u[i];
+                    else o[i] = u[i] > 0.0f ? o[i] : 0.0f;
+                }
+            }
+            Ck::store(c.out, chunk, o);
+        }
+    }
+}
+
+// The same for sums that are the result: n of them, n % 4 == 0.
+__global__ __launch_bounds__(256) void join_sums_kernel(const float *__restrict__ part, int parts,
+                                                        int64_t part_size, int64_t n,
+                                                        float *__restrict__ out) {
+    for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < n;
+         i += (int64_t)gridDim.x * 1024) {
+        float4 sum = *reinterpret_cast<const float4 *>(part + i);
+#pragma unroll 8
+        for (int p = 1; p < parts; ++p) {
+            const float4 x = *reinterpret_cast<const float4 *>(part + p * part_size + i);
+            sum.x += x.x, sum.y += x.y, sum.z += x.z, sum.w += x.w;
+        }
+        *reinterpret_cast<float4 *>(out + i) = sum;
+    }
+}
+
 // db_e: column sums of dy over each expert's rows. A block for 128 bytes of an expert's
-// columns: eight lanes take a row's eight chunks, 32 rows in turn over four waves.
+// columns: eight lanes take a row's eight chunks, 32 rows in turn over four waves; blockIdx.z
+// its part of the rows, for part_size results each.
 template <bool BF16>
 __global__ __launch_bounds__(256) void row_sums_kernel(const void *__restrict__ dy,
                                                        const int32_t *__restrict__ offsets,
-                                                       float *__restrict__ db, int N, int O) {
+                                                       float *__restrict__ db, int N, int O,
+                                                       int64_t part_size) {
     using Ck = RowChunk<BF16>;
     __shared__ float lds[32][8 * Ck::kN + 1];
     const int e = blockIdx.y;
     const int ncs = O / Ck::kN;
     const int g = threadIdx.x / 8;
-    const int a = row_bound(offsets, e, N), z = row_bound(offsets, e + 1, N);
+    const int a0 = row_bound(offsets, e, N), z0 = row_bound(offsets, e + 1, N);
+    const int64_t per = z0 > a0 ? (z0 - a0 - 1) / (int)gridDim.z + 1 : 0;
+    const int64_t a = a0 + blockIdx.z * per;
+    const int64_t z = a + per < z0 ? a + per : z0;
+    db += blockIdx.z * part_size;
     for (int c0 = blockIdx.x * 8; c0 < ncs; c0 += gridDim.x * 8) {
         const int c = c0 + threadIdx.x % 8;
         float s[Ck::kN];
@@ -787,13 +885,18 @@ __global__ __launch_bounds__(256) void row_sums_kernel(const void *__restrict__ 
     }
 }
 
-template <class In, int kForm, int BM, int BN, int WM, int WN, int kStages, bool kWide>
+enum { kEach, kWide, kInParts };   // a block per tile; per compute unit; per part of a tile
+
+template <class In, int kForm, int BM, int BN, int WM, int WN, int kStages, int kHow>
 hipError_t launch_tiles(const LinearCall &c, hipStream_t s) {
-    const size_t lds = kStages * (size_t)(BM + BN) * kChunk + (kWide ? (size_t)(c.E + 1) * 4 : 0);
+    const size_t lds =
+        kStages * (size_t)(BM + BN) * kChunk + (kHow == kWide ? (size_t)(c.E + 1) * 4 : 0);
     const void *kernel;
-    if constexpr (kWide) kernel = (const void *)&linear_wide_kernel<In, kForm, BM, BN, WM, WN, kStages>;
-    else kernel = (const void *)&linear_kernel<In, kForm, BM, BN, WM, WN, kStages>;
-    if (kStages * (BM + BN) * kChunk > 65536 || kWide) {   // opted in once per device
+    if constexpr (kHow == kWide)
+        kernel = (const void *)&linear_wide_kernel<In, kForm, BM, BN, WM, WN, kStages>;
+    else
+        kernel = (const void *)&linear_kernel<In, kForm, BM, BN, WM, WN, kStages, kHow == kInParts>;
+    if (kStages * (BM + BN) * kChunk > 65536 || kHow == kWide) {   // opted in once per device
         static std::mutex m;
         static bool granted[64] = {};
         int dev = 0;
@@ -807,15 +910,17 @@ hipError_t launch_tiles(const LinearCall &c, hipStream_t s) {
         }
     }
     int64_t blocks = kUnitsOfDevice;
-    if (!kWide) {
+    LinearCall call = c;
+    if (kHow != kWide) {
         const int64_t nn = ((kForm == kNT ? c.O : c.K) + BN - 1) / BN;
         const int64_t nm = (c.O + BM - 1) / BM;
         if (kForm != kTN) blocks = nn * ((int64_t)c.N / BM + (c.E < c.N ? c.E : c.N));
         else blocks = nm * nn >= 32 ? (nm * nn + 7) / 8 * 8 * c.E : nm * nn * c.E;
         blocks = (blocks + 7) / 8 * 8;
+        call.per_part = (int)blocks;
+        if (kHow == kInParts) blocks *= c.parts;
     }
     constexpr int64_t kMost = 1 << 22;   // a launch has fewer than 2^32 threads
-    LinearCall call = c;
     for (int64_t b = 0; b < blocks; b += kMost) {
         call.block0 = (int)b;
         void *args[] = {&call};
@@ -870,83 +975,192 @@ int pick_tile(int64_t N, int64_t E, int64_t cols) {
     return best;
 }
 
+// Parts of the contraction, for a call with few tiles and a long contraction: as many as give
+// every compute unit a tile, of four chunks at least, where that saves more than the sums' way
+// through memory and the launch that joins them. Tiles of 64 x 64 (kTN: 128 x 128, fp32
+// 64 x 128), with the time of a chunk of a tile alone on a unit. In one piece and in parts, us:
+// y of 1 row x 8192 to 512 in 32 parts 40 and 14 (fp32 165 and 18), of 512 x 4096 to 256 in 6
+// 23 and 12 (80 and 23); dx of 150 x 6152 to 1032 in 3 72 and 31 (121 and 48); dW 200 x 64 of
+// 5000 rows in 19 67 and 15 (188 and 20). What the rule leaves whole: dx of 1 x 512 to 2048,
+// 5.8, in 2 parts 7.1.
+int parts_of(int form, bool bf16, int64_t N, int64_t E, int64_t K, int64_t O) {
+    const int64_t steps = kChunk / (bf16 ? 2 : 4);
+    const int64_t experts = E < N ? E : N;
+    const int64_t cols = form == kNT ? O : K;
+    const int64_t bm = form == kTN && bf16 ? 128 : 64, bn = form == kTN ? 128 : 64;
+    const double us = form == kTN ? (bf16 ? 0.85 : 1.05) : (bf16 ? 0.36 : 0.6);
+    const int64_t rows = form == kTN ? E * ((O + bm - 1) / bm) : N / bm + experts;
+    const int64_t tiles = rows * ((cols + bn - 1) / bn);
+    const int64_t chunks = ((form == kNT ? K : form == kNN ? O : N / experts) + steps - 1) / steps;
+    int64_t parts = kUnitsOfDevice / tiles;
+    if (parts > chunks / 4) parts = chunks / 4;
+    if (parts > 32) parts = 32;
+    if (parts < 2) return 1;
+    const double results = form == kTN ? (double)E * O * K : (double)N * cols;
+    const double saved = chunks * us * (1.0 - 1.0 / parts);
+    const double spent = 4.0 + 8.0 * parts * results / 4e6;
+    return saved > 1.3 * spent ? (int)parts : 1;
+}
+
+// Parts of the rows whose sums are db: blocks for the whole device, of 256 rows at least (two
+// parts of 128 rows cost 1.5 us more than one of 256).
+int sum_parts(bool bf16, int64_t N, int64_t E, int64_t O) {
+    const int64_t blocks = (O * (bf16 ? 2 : 4) + 127) / 128 * E;
+    int64_t parts = 2 * kUnitsOfDevice / blocks;
+    if (parts > N / E / 256) parts = N / E / 256;
+    return parts < 4 ? 1 : parts > 64 ? 64 : (int)parts;
+}
+
 template <class In, int kForm>
 hipError_t launch_form(const LinearCall &c, hipStream_t s) {
     const int64_t avg = c.N / c.E;
+    if (c.parts > 1) {
+        if constexpr (kForm != kTN) return launch_tiles<In, kForm, 64, 64, 2, 2, 3, kInParts>(c, s);
+        else if constexpr (In::kBf16) return launch_tiles<In, kForm, 128, 128, 2, 2, 2, kInParts>(c, s);
+        else return launch_tiles<In, kForm, 64, 128, 2, 2, 2, kInParts>(c, s);
+    }
     if constexpr (kForm == kTN) {
         // A tile stores its matrix's part once and multiplies little, so the tile matters
         // for experts with many rows only (64 experts, 4096 x 1024: 64 rows of 128 x 128 and
         // 256 x 256 tiles 212 and 229 us, 8192 rows 367 and 357, 16384 rows 498 and 478).
         if constexpr (!In::kBf16) {
-            return launch_tiles<F32, kTN, 64, 128, 2, 2, 2, false>(c, s);
+            return launch_tiles<F32, kTN, 64, 128, 2, 2, 2, kEach>(c, s);
         } else {
             const int64_t tiles = (int64_t)c.E * ((c.O + 255) / 256) * ((c.K + 255) / 256);
             if (avg >= 96 && tiles >= 192)
-                return launch_tiles<Bf16, kTN, 256, 256, 2, 4, 2, true>(c, s);
-            return launch_tiles<Bf16, kTN, 128, 128, 2, 2, 2, false>(c, s);
+                return launch_tiles<Bf16, kTN, 256, 256, 2, 4, 2, kWide>(c, s);
+            return launch_tiles<Bf16, kTN, 128, 128, 2, 2, 2, kEach>(c, s);
         }
     } else if constexpr (!In::kBf16) {
         // Few rows: as much in flight as possible (512 rows of 64 experts, 1024 to 2048: 119 us,
         // 64 x 128 142).
-        if (avg < 32) return launch_tiles<F32, kForm, 32, 128, 1, 4, 3, false>(c, s);
+        if (avg < 32) return launch_tiles<F32, kForm, 32, 128, 1, 4, 3, kEach>(c, s);
         const int64_t tiles =
             (c.N / 64 + c.E / 2) * (((kForm == kNT ? c.O : c.K) + 127) / 128);
-        if (tiles < 4 * kUnitsOfDevice) return launch_tiles<F32, kForm, 64, 64, 2, 2, 2, false>(c, s);
-        return launch_tiles<F32, kForm, 64, 128, 2, 2, 2, false>(c, s);
+        if (tiles < 4 * kUnitsOfDevice) return launch_tiles<F32, kForm, 64, 64, 2, 2, 2, kEach>(c, s);
+        return launch_tiles<F32, kForm, 64, 128, 2, 2, 2, kEach>(c, s);
     } else {
         // A few rows: the matrices' bytes count, and what keeps most of them in flight (64 rows
         // of 64 experts, 1024 to 4096: 58.6 us, 64 x 128 tiles 60.8; of 16, 2048 to 8192: 96 and
         // 121). By columns a row of 32 x 64 tiles reads too short pieces, but for single rows.
         if constexpr (kForm == kNT)
             if (avg <= 16)
-                return launch_tiles<Bf16, kForm, 32, 64, 1, 2, 4, false>(c, s);
+                return launch_tiles<Bf16, kForm, 32, 64, 1, 2, 4, kEach>(c, s);
         if constexpr (kForm == kNN)
             if (avg <= 2)
-                return launch_tiles<Bf16, kForm, 32, 64, 1, 2, 2, false>(c, s);
+                return launch_tiles<Bf16, kForm, 32, 64, 1, 2, 2, kEach>(c, s);
         switch (pick_tile(c.N, c.E, kForm == kNT ? c.O : c.K)) {
-            case 0: return launch_tiles<Bf16, kForm, 64, 128, 2, 2, 2, false>(c, s);
-            case 1: return launch_tiles<Bf16, kForm, 128, 128, 2, 2, 2, false>(c, s);
-            case 2: return launch_tiles<Bf16, kForm, 256, 256, 2, 4, 2, true>(c, s);
-            default: return launch_tiles<Bf16, kForm, 64, 64, 2, 2, 3, false>(c, s);
+            case 0: return launch_tiles<Bf16, kForm, 64, 128, 2, 2, 2, kEach>(c, s);
+            case 1: return launch_tiles<Bf16, kForm, 128, 128, 2, 2, 2, kEach>(c, s);
+            case 2: return launch_tiles<Bf16, kForm, 256, 256, 2, 4, 2, kWide>(c, s);
+            default: return launch_tiles<Bf16, kForm, 64, 64, 2, 2, 3, kEach>(c, s);
         }
     }
 }
 
+// The call, or its parts into the workspace and their join.
+template <class In, int kForm>
+hipError_t launch_call(LinearCall c, void *workspace, hipStream_t s) {
+    c.parts = parts_of(kForm, In::kBf16, c.N, c.E, c.K, c.O);
+    if (c.parts == 1) return launch_form<In, kForm>(c, s);
+    void *out = c.out;
+    const float *part = static_cast<const float *>(workspace);
+    const int64_t cols = kForm == kNT ? c.O : c.K;
+    c.part_size = (kForm == kTN ? (int64_t)c.E * c.O : (int64_t)c.N) * cols;
+    c.out = workspace;
+    hipError_t err = launch_form<In, kForm>(c, s);
+    if (err != hipSuccess) return err;
+    c.out = out;
+    constexpr int64_t kMost = 1 << 20;
+    if constexpr (kForm == kTN) {
+        const int64_t blocks = (c.part_size + 1023) / 1024;
+        hipLaunchKernelGGL(join_sums_kernel, dim3((unsigned)(blocks < kMost ? blocks : kMost)),
+                           dim3(256), 0, s, part, c.parts, c.part_size, c.part_size,
+                           static_cast<float *>(out));
+    } else {
+        const int64_t blocks = ((int64_t)c.N * ((cols + 511) / 512) + 3) / 4;
+        hipLaunchKernelGGL((join_rows_kernel<In, kForm>),
+                           dim3((unsigned)(blocks < kMost ? blocks : kMost)), dim3(256), 0, s, c,
+                           part);
+    }
+    return hipGetLastError();
+}
+
 template <int kForm>
-hipError_t launch(const LinearCall &c, int bf16, hipStream_t s) {
-    return bf16 ? launch_form<Bf16, kForm>(c, s) : launch_form<F32, kForm>(c, s);
+hipError_t launch(const LinearCall &c, int bf16, void *workspace, hipStream_t s) {
+    return bf16 ? launch_call<Bf16, kForm>(c, workspace, s)
+                : launch_call<F32, kForm>(c, workspace, s);
+}
+
+LinearCall call_of(const void *A, const void *B, const void *bias, const void *extra,
+                   const int32_t *offsets, void *out, int64_t N, int64_t E, int64_t K, int64_t O,
+                   int relu) {
+    LinearCall c{};
+    c.A = A;
+    c.B = B;
+    c.bias = bias;
+    c.extra = extra;
+    c.offsets = offsets;
+    c.out = out;
+    c.N = (int)N;
+    c.E = (int)E;
+    c.K = (int)K;
+    c.O = (int)O;
+    c.relu = relu;
+    return c;
+}
+
+// fp32 sums of a call's parts: of the products, then (dW) those of db.
+int64_t part_sums(int form, bool bf16, int64_t N, int64_t E, int64_t K, int64_t O) {
+    const int64_t parts = parts_of(form, bf16, N, E, K, O);
+    return parts == 1 ? 0 : parts * (form == kNT ? N * O : form == kNN ? N * K : E * O * K);
 }
 
 }  // namespace
 
+size_t linear_workspace_size(int product, int64_t N, int64_t E, int64_t K, int64_t O, int bf16) {
+    int64_t n = part_sums(product, bf16 != 0, N, E, K, O);
+    if (product == kTN) {
+        const int64_t parts = sum_parts(bf16 != 0, N, E, O);
+        if (parts > 1) n += parts * E * O;
+    }
+    return ((size_t)n * 4 + 255) / 256 * 256;
+}
+
 hipError_t launch_linear(const void *x, const void *w, const void *bias, const void *residual,
                          const int32_t *offsets, void *y, int64_t N, int64_t E, int64_t K,
-                         int64_t O, int relu, int bf16, hipStream_t s) {
-    return launch<kNT>({x, w, bias, residual, offsets, y, (int)N, (int)E, (int)K, (int)O, relu, 0},
-                            bf16, s);
+                         int64_t O, int relu, int bf16, void *workspace, hipStream_t s) {
+    return launch<kNT>(call_of(x, w, bias, residual, offsets, y, N, E, K, O, relu), bf16, workspace,
+                       s);
 }
 
 hipError_t launch_linear_dx(const void *dy, const void *w, const void *relu_of,
                             const int32_t *offsets, void *dx, int64_t N, int64_t E, int64_t K,
-                            int64_t O, int bf16, hipStream_t s) {
-    return launch<kNN>({dy, w, nullptr, relu_of, offsets, dx, (int)N, (int)E, (int)K, (int)O, 0, 0},
-                            bf16, s);
+                            int64_t O, int bf16, void *workspace, hipStream_t s) {
+    return launch<kNN>(call_of(dy, w, nullptr, relu_of, offsets, dx, N, E, K, O, 0), bf16,
+                       workspace, s);
 }
 
 hipError_t launch_linear_dw(const void *dy, const void *x, const int32_t *offsets, float *dw,
                             float *db, int64_t N, int64_t E, int64_t K, int64_t O, int bf16,
-                            hipStream_t s) {
+                            void *workspace, hipStream_t s) {
     const hipError_t err = launch<kTN>(
-        {dy, x, nullptr, nullptr, offsets, dw, (int)N, (int)E, (int)K, (int)O, 0, 0}, bf16, s);
+        call_of(dy, x, nullptr, nullptr, offsets, dw, N, E, K, O, 0), bf16, workspace, s);
     if (err != hipSuccess || db == nullptr) return err;
-    const int64_t parts = (O * (bf16 ? 2 : 4) + 127) / 128;
-    const dim3 grid((unsigned)(parts < 1024 ? parts : 1024), (unsigned)E);
+    const int parts = sum_parts(bf16 != 0, N, E, O);
+    float *sums = db;
+    if (parts > 1) sums = static_cast<float *>(workspace) + part_sums(kTN, bf16 != 0, N, E, K, O);
+    const int64_t blocks = (O * (bf16 ? 2 : 4) + 127) / 128;
+    const dim3 grid((unsigned)(blocks < 1024 ? blocks : 1024), (unsigned)E, (unsigned)parts);
     if (bf16)
-        hipLaunchKernelGGL(row_sums_kernel<true>, grid, dim3(256), 0, s, dy, offsets, db, (int)N,
-                           (int)O);
+        hipLaunchKernelGGL(row_sums_kernel<true>, grid, dim3(256), 0, s, dy, offsets, sums, (int)N,
+                           (int)O, E * O);
     else
-        hipLaunchKernelGGL(row_sums_kernel<false>, grid, dim3(256), 0, s, dy, offsets, db, (int)N,
-                           (int)O);
+        hipLaunchKernelGGL(row_sums_kernel<false>, grid, dim3(256), 0, s, dy, offsets, sums, (int)N,
+                           (int)O, E * O);
+    if (parts > 1)
+        hipLaunchKernelGGL(join_sums_kernel, dim3((unsigned)((E * O + 1023) / 1024)), dim3(256), 0,
+                           s, sums, parts, E * O, E * O, db);
     return hipGetLastError();
 }
 

@@ -28,7 +28,8 @@ from __future__ import annotations
 import contextlib
 import dataclasses
 
-from . import _check, _dtype_code, _stream_ptr, _torch, lib
+from . import (BASE_PRODUCT_DW, BASE_PRODUCT_DX, BASE_PRODUCT_Y, _check, _dtype_code, _stream_ptr,
+               _torch, lib)
 
 
 @dataclasses.dataclass
@@ -329,6 +330,21 @@ def expert_norm_backward(dy, x, weight, mean, rstd, offsets=None, perm=None, k: 
     return out, dweight, dbias
 
 
+def expert_linear_workspace_size(product: int, N: int, E: int, K: int, O: int, dtype: int) -> int:
+    """Bytes for a BASE_PRODUCT_* of these sizes and BASE_* type; 0 for most."""
+    return int(lib().base_expert_linear_workspace_size(product, N, E, K, O, dtype))
+
+
+def _linear_workspace(workspace, product, N, E, K, O, dtype, device):
+    """(tensor or None, address, bytes)."""
+    if workspace is None:
+        n = expert_linear_workspace_size(product, N, E, K, O, dtype)
+        if n == 0:
+            return None, None, 0
+        workspace = _workspace(n, device)
+    return workspace, workspace.data_ptr(), workspace.nbytes
+
+
 def _linear_args(w, offsets, **others):
     torch = _torch()
     _need(w=w, offsets=offsets, **others)
@@ -339,11 +355,12 @@ def _linear_args(w, offsets, **others):
 
 
 def expert_linear(x, w, offsets, bias=None, relu: bool = False, residual=None, out=None,
-                  stream=None):
+                  workspace=None, stream=None):
     """Routed rows x [N, K] times their experts' matrices w [E, O, K]: y = act(x w^T +
     bias) + residual, act the ReLU with `relu` (base_expert_linear)."""
     torch = _torch()
-    E, O, K = _linear_args(w, offsets, x=x, bias=bias, residual=residual, out=out)
+    E, O, K = _linear_args(w, offsets, x=x, bias=bias, residual=residual, out=out,
+                           workspace=workspace)
     _dims("x", x, 2)
     N = x.shape[0]
     _like("x", x, (N, K), w.dtype)
@@ -353,18 +370,20 @@ def expert_linear(x, w, offsets, bias=None, relu: bool = False, residual=None, o
     with _on(stream):
         if out is None:
             out = _empty(N, O, x.dtype, x.device)
+        code = _dtype_code(x)
+        ws, at, n = _linear_workspace(workspace, BASE_PRODUCT_Y, N, E, K, O, code, x.device)
         _check(lib().base_expert_linear(x.data_ptr(), w.data_ptr(), _ptr(bias), _ptr(residual),
                                         offsets.data_ptr(), out.data_ptr(), N, E, K, O,
-                                        1 if relu else 0, _dtype_code(x), _stream_ptr(stream)),
+                                        1 if relu else 0, code, at, n, _stream_ptr(stream)),
                "base_expert_linear")
     return out
 
 
-def expert_linear_dx(dy, w, offsets, relu_of=None, out=None, stream=None):
+def expert_linear_dx(dy, w, offsets, relu_of=None, out=None, workspace=None, stream=None):
     """Gradient of expert_linear by its rows, dy w (base_expert_linear_dx). With relu_of
     (the ReLU's result that was x) the gradient before that ReLU: 0 where it is not > 0."""
     torch = _torch()
-    E, O, K = _linear_args(w, offsets, dy=dy, relu_of=relu_of, out=out)
+    E, O, K = _linear_args(w, offsets, dy=dy, relu_of=relu_of, out=out, workspace=workspace)
     _dims("dy", dy, 2)
     N = dy.shape[0]
     _like("dy", dy, (N, O), w.dtype)
@@ -373,18 +392,20 @@ def expert_linear_dx(dy, w, offsets, relu_of=None, out=None, stream=None):
     with _on(stream):
         if out is None:
             out = _empty(N, K, dy.dtype, dy.device)
+        code = _dtype_code(dy)
+        ws, at, n = _linear_workspace(workspace, BASE_PRODUCT_DX, N, E, K, O, code, dy.device)
         _check(lib().base_expert_linear_dx(dy.data_ptr(), w.data_ptr(), _ptr(relu_of),
-                                           offsets.data_ptr(), out.data_ptr(), N, E, K, O,
-                                           _dtype_code(dy), _stream_ptr(stream)),
+                                           offsets.data_ptr(), out.data_ptr(), N, E, K, O, code,
+                                           at, n, _stream_ptr(stream)),
                "base_expert_linear_dx")
     return out
 
 
-def expert_linear_dw(dy, x, offsets, stream=None):
+def expert_linear_dw(dy, x, offsets, workspace=None, stream=None):
     """Gradient of expert_linear by its matrices and bias (base_expert_linear_dw):
     (dw float32 [E, O, K], db float32 [E, O]), summed over each expert's rows."""
     torch = _torch()
-    _need(dy=dy, x=x, offsets=offsets)
+    _need(dy=dy, x=x, offsets=offsets, workspace=workspace)
     _dims("dy", dy, 2)
     _dims("x", x, 2)
     _dims("offsets", offsets, 1)
@@ -394,8 +415,10 @@ def expert_linear_dw(dy, x, offsets, stream=None):
     with _on(stream):
         dw = torch.empty((E, O, K), dtype=torch.float32, device=dy.device)
         db = _empty(E, O, torch.float32, dy.device)
+        code = _dtype_code(dy)
+        ws, at, n = _linear_workspace(workspace, BASE_PRODUCT_DW, N, E, K, O, code, dy.device)
         _check(lib().base_expert_linear_dw(dy.data_ptr(), x.data_ptr(), offsets.data_ptr(),
-                                           dw.data_ptr(), db.data_ptr(), N, E, K, O,
-                                           _dtype_code(dy), _stream_ptr(stream)),
+                                           dw.data_ptr(), db.data_ptr(), N, E, K, O, code, at, n,
+                                           _stream_ptr(stream)),
                "base_expert_linear_dw")
     return dw, db

@@ -105,7 +105,7 @@ def test_products(L):
     big = 1 << 28   # apart, each smaller than this
     at = [FAKE + i * big for i in range(6)]
     g = dict(x=at[0], w=at[1], bias=None, residual=None, offsets=at[2], y=at[3], N=4, E=2, K=16,
-             O=24, relu=0, dtype=BF16, stream=None)
+             O=24, relu=0, dtype=BF16, ws=None, wsb=0, stream=None)
     f = L.base_expert_linear
     for bad in (dict(x=None), dict(w=None), dict(offsets=None), dict(y=None), dict(N=0), dict(E=0),
                 dict(K=12), dict(O=20), dict(relu=2), dict(y=at[0] + 32), dict(y=at[1] + 64),
@@ -114,17 +114,38 @@ def test_products(L):
     assert call(f, g, dtype=pb.BASE_I16) == DT
     assert call(f, g, E=2049) == RNG and call(f, g, K=(1 << 20) + 8) == RNG
     g = dict(dy=at[0], w=at[1], relu_of=None, offsets=at[2], dx=at[3], N=4, E=2, K=16, O=24,
-             dtype=F32, stream=None)
+             dtype=F32, ws=None, wsb=0, stream=None)
     f = L.base_expert_linear_dx
     for bad in (dict(dy=None), dict(w=None), dict(offsets=None), dict(dx=None), dict(dx=at[0]),
                 dict(relu_of=at[3] + 32), dict(O=4)):
         assert call(f, g, **bad) == INV, bad
     g = dict(dy=at[0], x=at[1], offsets=at[2], dw=at[3], db=at[4], N=4, E=2, K=16, O=24, dtype=F32,
-             stream=None)
+             ws=None, wsb=0, stream=None)
     f = L.base_expert_linear_dw
     for bad in (dict(dy=None), dict(x=None), dict(offsets=None), dict(dw=None), dict(dw=at[1] + 16),
                 dict(db=at[3] + 16), dict(K=-8)):
         assert call(f, g, **bad) == INV, bad
+
+
+def test_products_workspace(L):
+    """Sums in parts need a workspace; whether a call cuts them goes by its sizes."""
+    size = pb.expert_linear_workspace_size
+    big = 1 << 28
+    at = [FAKE + i * big for i in range(6)]
+    cut = dict(N=64, E=1, K=8192, O=512)
+    for product, dtype in ((pb.BASE_PRODUCT_Y, BF16), (pb.BASE_PRODUCT_Y, F32)):
+        n = size(product, *cut.values(), dtype)
+        assert n > 0 and n % 256 == 0
+        g = dict(x=at[0], w=at[1], bias=None, residual=None, offsets=at[2], y=at[3], **cut, relu=0,
+                 dtype=dtype, ws=at[4], wsb=n - 1, stream=None)
+        assert call(L.base_expert_linear, g) == WS
+        assert call(L.base_expert_linear, g, ws=None, wsb=n) == WS
+        assert call(L.base_expert_linear, g, ws=at[4] + 16, wsb=n) == WS
+    assert size(pb.BASE_PRODUCT_DW, 8192, 2, 512, 256, BF16) > 0
+    assert size(pb.BASE_PRODUCT_DX, 64, 1, 512, 8192, F32) > 0
+    assert size(pb.BASE_PRODUCT_Y, 32768, 32, 2048, 8192, BF16) == 0
+    assert size(3, *cut.values(), BF16) == 0 and size(0, 0, 1, 8, 8, BF16) == 0
+    assert size(0, 64, 1, 8192, 12, BF16) == 0
 
 
 def test_binding_refuses_host_tensors():

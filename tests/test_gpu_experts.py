@@ -325,6 +325,46 @@ def test_products(N, E, K, O, dtype):
     assert torch.equal(again[0], dw) and torch.equal(again[1], db)
 
 
+# Few outputs and long sums: cut into parts (the number of them is in the comment, a product's
+# y, dx, dw and db in bf16 and fp32).
+IN_PARTS = [(1, 1, 8192, 512),      # y 32, 32; one row, parts of four chunks
+            (70, 1, 8192, 264),     # y 25, 25; uneven parts, columns behind 256
+            (40, 3, 4104, 72),      # y 16, 32; a part of part of a chunk, the last ones empty
+            (130, 1, 8, 4096),      # dx 16, 32
+            (150, 2, 1032, 6152),   # dx 3, 3; three groups of columns in the join
+            (300, 2, 8192, 136),    # y 14, 14; several tiles of rows
+            (5000, 3, 264, 40),     # dw 6, 13; db 6, 6
+            (5000, 1, 64, 200)]     # dw 19, 32; db 19, 19
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("N,E,K,O", IN_PARTS)
+def test_products_in_parts(N, E, K, O, dtype):
+    code = pb.BASE_F32 if dtype == "f32" else pb.BASE_BF16
+    sizes = [pb.expert_linear_workspace_size(p, N, E, K, O, code)
+             for p in (pb.BASE_PRODUCT_Y, pb.BASE_PRODUCT_DX, pb.BASE_PRODUCT_DW)]
+    assert max(sizes) > 0
+    test_products(N, E, K, O, dtype)
+    # the workspace's contents do not matter, and another expert's rows may be none or all
+    r = rng_of(N, E, K, O, 1)
+    x, w, dy = (dev(rows(r, n, dtype)[1]) for n in ((N, K), (E, O, K), (N, O)))
+    off = dev(np.array([0] * E + [N], dtype=np.int32))
+    got = []
+    for fill in (0, 255):
+        ws = [torch.full((max(n, 256),), fill, dtype=torch.uint8, device="cuda") for n in sizes]
+        got.append((pb.expert_linear(x, w, off, workspace=ws[0]),
+                    pb.expert_linear_dx(dy, w, off, workspace=ws[1]),
+                    *pb.expert_linear_dw(dy, x, off, workspace=ws[2])))
+    for a, b in zip(*got):
+        assert torch.equal(a, b) and bool(torch.isfinite(a).all())
+    y, dx, dw, db = got[0]
+    assert bool((dw[:-1] == 0).all()) and bool((db[:-1] == 0).all())
+    step = STEP[dtype]
+    near_product(y, x, w[-1].t().contiguous(), K, step)
+    near_product(dx, dy, w[-1], O, step)
+    near_product(dw[-1], dy.t().contiguous(), x, N, U)
+
+
 def test_products_keep_infinities_and_nan_in_their_rows():
     """A row of NaN or infinities spoils its own results only, and the ReLU keeps a NaN."""
     r = rng_of(11)
