@@ -975,14 +975,15 @@ int pick_tile(int64_t N, int64_t E, int64_t cols) {
     return best;
 }
 
-// Parts of the contraction, for a call with few tiles and a long contraction: as many as give
-// every compute unit a tile, of four chunks at least, where that saves more than the sums' way
-// through memory and the launch that joins them. Tiles of 64 x 64 (kTN: 128 x 128, fp32
-// 64 x 128), with the time of a chunk of a tile alone on a unit. In one piece and in parts, us:
-// y of 1 row x 8192 to 512 in 32 parts 40 and 14 (fp32 165 and 18), of 512 x 4096 to 256 in 6
-// 23 and 12 (80 and 23); dx of 150 x 6152 to 1032 in 3 72 and 31 (121 and 48); dW 200 x 64 of
-// 5000 rows in 19 67 and 15 (188 and 20). What the rule leaves whole: dx of 1 x 512 to 2048,
-// 5.8, in 2 parts 7.1.
+// Parts of the contraction, for a call whose tiles do not fill the device once: of four chunks
+// at least, as many as bring the least time of whole rounds of tiles over the compute units
+// with the sums' way through memory and the launch that joins them. Tiles of 64 x 64 (kTN:
+// 128 x 128, fp32 64 x 128), with the time of a chunk of a tile alone on a unit. In one piece
+// and in parts, us: y of 1 row x 8192 to 512 in 32 parts 40 and 14 (fp32 165 and 18), of
+// 512 x 4096 to 256 in 6 23 and 12 (80 and 23); dx of 150 x 6152 to 1032 in 7 72 and 21 (121
+// and 41); dW 200 x 64 of 5000 rows in 19 67 and 15 (in 32 188 and 20), fp32 216 x 1672 of 8606
+// rows, three experts, in 3 109 and 76. What the rule leaves whole: dx of 1 x 512 to 2048, 5.8,
+// in 2 parts 7.1.
 int parts_of(int form, bool bf16, int64_t N, int64_t E, int64_t K, int64_t O) {
     const int64_t steps = kChunk / (bf16 ? 2 : 4);
     const int64_t experts = E < N ? E : N;
@@ -992,14 +993,20 @@ int parts_of(int form, bool bf16, int64_t N, int64_t E, int64_t K, int64_t O) {
     const int64_t rows = form == kTN ? E * ((O + bm - 1) / bm) : N / bm + experts;
     const int64_t tiles = rows * ((cols + bn - 1) / bn);
     const int64_t chunks = ((form == kNT ? K : form == kNN ? O : N / experts) + steps - 1) / steps;
-    int64_t parts = kUnitsOfDevice / tiles;
-    if (parts > chunks / 4) parts = chunks / 4;
-    if (parts > 32) parts = 32;
-    if (parts < 2) return 1;
+    if (tiles > kUnitsOfDevice) return 1;
     const double results = form == kTN ? (double)E * O * K : (double)N * cols;
-    const double saved = chunks * us * (1.0 - 1.0 / parts);
-    const double spent = 4.0 + 8.0 * parts * results / 4e6;
-    return saved > 1.3 * spent ? (int)parts : 1;
+    const int64_t most = chunks / 4 < 32 ? chunks / 4 : 32;
+    int best = 1;
+    double low = chunks * us;
+    for (int64_t p = 2; p <= most; ++p) {
+        const int64_t rounds = (tiles * p + kUnitsOfDevice - 1) / kUnitsOfDevice;
+        const double cost = rounds * chunks * us / p + 1.3 * (4.0 + 8.0 * p * results / 4e6);
+        if (cost < low) {
+            best = (int)p;
+            low = cost;
+        }
+    }
+    return best;
 }
 
 // Parts of the rows whose sums are db: blocks for the whole device, of 256 rows at least (two
