@@ -280,6 +280,10 @@ struct Tiles {
     static constexpr int kLoads = StageA::kSlots + StageB::kSlots;   // of a wave, per stage
     static constexpr bool kSums = kForm == kTN || kPartial;   // results stored as fp32 sums
     static constexpr int kOutSize = kSums ? 4 : (int)kSize;
+    // fp32 sums are stored 128 bytes of a row at once, 4 to a lane (16 bytes to a lane take 32
+    // of a row: dW 4096 x 1024 of 64 experts, 64 rows 216 us, 201 so; 4096 rows 251 and 242).
+    // Not by 256 x 256 tiles, which wait for the number of their stores (16384 rows 412, 509).
+    static constexpr bool kByRow = kSums && BM < 256;
 
     const LinearCall &c;
     char *lds;
@@ -396,7 +400,8 @@ struct Tiles {
                 for (int j = 0; j < TN; ++j)
 #pragma unroll
                     for (int x = 0; x < X; ++x)
-                        acc[x][j] = In::mma(b[set][j], a[set][x], acc[x][j], i);
+                        acc[x][j] = kByRow ? In::mma(a[set][x], b[set][j], acc[x][j], i)
+                                           : In::mma(b[set][j], a[set][x], acc[x][j], i);
         };
         barrier();
         if (nk > 0) fetch(0, lds, 0);
@@ -480,13 +485,14 @@ struct Tiles {
         }
     };
 
-    // Stores of a wave per 32 x 32 results, 16 bytes a lane each.
+    // Stores of a wave per 32 x 32 results, of 16 bytes a lane each.
     static constexpr int kStores = 16 * kOutSize / 16;
 
     // What follows the product, and the stores. 32x32 results: lane holds row lane % 32;
-    // register i column 8 (i / 4) + 4 (lane / 32) + i % 4. kNT and kNN exchange halves between
-    // the half waves, so that a lane has eight neighbouring columns. Lanes outside the
-    // result store to nowhere, so that every wave issues the same number of stores.
+    // register i column 8 (i / 4) + 4 (lane / 32) + i % 4; kByRow the other way round. kNT and
+    // kNN exchange halves between the half waves, so that a lane has eight neighbouring
+    // columns. Lanes outside the result store to nowhere, so that every wave issues the same
+    // number of stores.
     template <int X>
     __device__ void finish(const Tile &d, f32x16_t (&acc)[X][TN], const Added<X> &added) const {
         const int half = lane >> 5;
@@ -501,7 +507,17 @@ struct Tiles {
 #pragma unroll
             for (int j = 0; j < TN; ++j) {
                 const int nj = d.n0 + 32 * (wn * TN + j);
-                if constexpr (kSums) {
+                if constexpr (kByRow) {
+                    const int n = nj + (lane & 31);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int m = 32 * (wm + WM * x) + 8 * (i / 4) + 4 * half + i % 4;
+                        const uint32_t at = ((uint32_t)m * cols + n) * 4;
+                        __builtin_amdgcn_raw_buffer_store_b32(
+                            __float_as_uint(acc[x][j][i]), rsrc,
+                            (int)(m < d.m_end - d.m0 && n < cols ? at : kNowhere), 0, 0);
+                    }
+                } else if constexpr (kSums) {
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
                         const int n = nj + 8 * q + 4 * half;
@@ -633,6 +649,7 @@ __device__ inline bool matrix_tile(const LinearCall &c, int block, Tile &t, bool
 template <class In, int kForm, int BM, int BN, int WM, int WN, int kStages>
 __global__ __launch_bounds__(64 * WM * WN, 1) void linear_wide_kernel(LinearCall c) {
     using G = Tiles<In, kForm, BM, BN, WM, WN, kStages>;
+    static_assert(!G::kByRow, "kStores is the number of stores");
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     G g(c, lds);
     // first[e]: row tiles of the experts before e; a thread for a run of experts.
