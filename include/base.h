@@ -537,7 +537,8 @@ int base_combine_backward(const void *dY, const void *F, const float *weights,
  *   dweight, dbias  [device] float32 [E, d], written entirely (zero for an
  *            expert without rows); dbias may be NULL
  *   eps      >= 0, finite
- *   workspace [device] base_expert_norm_workspace_size(N, E, d) bytes, 256-aligned
+ *   workspace [device] base_expert_norm_workspace_size(N, E, d) bytes, 256-aligned; any
+ *            contents at entry. Calls that overlap in time need their own.
  *   N < 2^31, E <= 2048, d % 8 == 0, d <= 16384; matrices 16-byte aligned. y and dx
  *   must not overlap x; dx may be dy or residual.
  * Mean, squares about the mean and all sums are fp32, in a fixed order.
@@ -574,8 +575,9 @@ int base_expert_norm_backward(const void *dy, const void *x, const int32_t *perm
  *   N < 2^31, E <= 2048, K % 8 == 0, O % 8 == 0, K, O <= 2^20; 16-byte aligned. y
  *   may be residual and dx may be relu_of; outputs overlap no other input.
  *   workspace [device] base_expert_linear_workspace_size(product, N, E, K, O, dtype)
- *      bytes, 256-aligned; any contents at entry. 0 (then workspace may be NULL) but for
- *      calls with few outputs and a long sum, which is cut into parts.
+ *      bytes, 256-aligned; any contents at entry. Calls that overlap in time need their
+ *      own. 0 (then workspace may be NULL) but for calls with few outputs and a long sum,
+ *      which is cut into parts.
  * Products are summed in fp32 (bf16 products are exact there; fp32 ones are not
  * reduced), in an order that depends on the sizes only: the same call gives the
  * same bits every time.

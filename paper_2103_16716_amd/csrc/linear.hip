@@ -144,8 +144,8 @@ struct Stage {
     uint32_t at[kSlots];   // offsets of this thread's slots from the chunk's first byte
     uint32_t unit;         // kAlong: this thread's unit of a row's chunk
 
-    // ld: bytes from a row (across: a step) to the next; across, rows is the number of
-    // result rows left in the matrix (kAlong: those past the end lie behind the buffer).
+    // ld: bytes from a row (across: a step) to the next; rows: the result rows left in the
+    // matrix (across only: along, those past the end lie behind the buffer).
     __device__ void init(int64_t ld, int rows) {
         const int tid = threadIdx.x;
         if constexpr (kAlong) {
@@ -184,18 +184,16 @@ struct Stage {
             return *reinterpret_cast<const unit_t *>(lds + r * kChunk +
                                                      (((2 * ks + half) ^ ((r >> 1) & 7)) * 16));
         } else if constexpr (In::kBf16) {
-            const int s = 8 * half + ((lane & 15) >> 2);   // (+ 16 ks + 4 for the second)
-            const int off = s * kRow + ((t ^ exchange(s)) * 4 + ((lane >> 3) & 2) + ((lane >> 1) & 1)) * 16 +
-                            (lane & 1) * 8 + 16 * ks * kRow;
-            const int s2 = s + 4;
-            const int off2 = s2 * kRow + ((t ^ exchange(s2)) * 4 + ((lane >> 3) & 2) + ((lane >> 1) & 1)) * 16 +
-                             (lane & 1) * 8 + 16 * ks * kRow;
+            const int s = 8 * half + ((lane & 15) >> 2);   // (+ 16 ks; + 4 for the second half)
+            const int in_row = ((lane >> 3) & 2) * 16 + ((lane >> 1) & 1) * 16 + (lane & 1) * 8;
+            BASE_LDS char *at = (BASE_LDS char *)lds + (16 * ks + s) * kRow + in_row;
             const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (BASE_LDS s16x4_t *)((BASE_LDS char *)lds + off));
+                (BASE_LDS s16x4_t *)(at + (t ^ exchange(s)) * 64));
             const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (BASE_LDS s16x4_t *)((BASE_LDS char *)lds + off2));
+                (BASE_LDS s16x4_t *)(at + 4 * kRow + (t ^ exchange(s + 4)) * 64));
             typedef short s16x8_t __attribute__((ext_vector_type(8)));
-            return __builtin_bit_cast(unit_t, (s16x8_t)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+            const s16x8_t v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+            return __builtin_bit_cast(unit_t, v);
         } else {
             unit_t v;
             const int s = 4 * (2 * ks + half);
@@ -346,8 +344,8 @@ struct Tiles {
     }
 
     // Operand reads go between the products of the step before, one to a product or every
-    // few: 32768 rows x 2048 to 8192, 32 experts 1035 -> 1010 us, by columns 1028 -> 1005. (Not for
-    // the matrices' gradient: 4096 rows of 64 experts, 1024 to 4096, 274 -> 306 us.)
+    // few: 32768 rows x 2048 to 8192, 32 experts 1035 -> 1010 us, by columns 1028 -> 1005. (Not
+    // for the matrices' gradient: 4096 rows of 64 experts, 1024 to 4096, 274 -> 306 us.)
     template <int X>
     __device__ static void interleave() {
         if constexpr (In::kBf16 && kForm != kTN) {
@@ -617,8 +615,9 @@ struct Tiles {
     }
 };
 
-// The tile of kTN that block number `block` computes: every expert's tiles are spread over the XCDs (an expert with many rows
-// would else hold up one of them), a run to each. Small matrices go round by block.
+// The tile of kTN that block number `block` computes: every expert's tiles are spread over the
+// XCDs (an expert with many rows would else hold up one of them), a run to each. Small matrices
+// go round by block.
 template <int BM, int BN>
 __device__ inline bool matrix_tile(const LinearCall &c, int block, Tile &t, bool &more) {
     const int nm = (c.O + BM - 1) / BM, nn = (c.K + BN - 1) / BN, all = nm * nn;
@@ -920,8 +919,9 @@ hipError_t launch_tiles(const LinearCall &c, hipStream_t s) {
         if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return hipErrorInvalidDevice;
         std::lock_guard<std::mutex> lock(m);
         if (!granted[dev]) {
-            const hipError_t err = hipFuncSetAttribute(
-                kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kStages * (BM + BN) * kChunk + 2049 * 4);
+            const hipError_t err =
+                hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize,
+                                    kStages * (BM + BN) * kChunk + 2049 * 4);
             if (err != hipSuccess) return err;
             granted[dev] = true;
         }
@@ -958,9 +958,9 @@ hipError_t launch_tiles(const LinearCall &c, hipStream_t s) {
 //   64 x 128   0.62  0.4   (4096, 64, 1024, 4096: 127 us, 128 x 128 131, 32 x 64 182)
 //   64 x 64    0.36  0.27  (512, 1, 2048, 2048: 13.7 us, 64 x 128 22.7, 256 x 256 52)
 // The 256 x 256 tiles are one to a unit: a started round of them takes a whole one's time,
-// or 0.6 or 0.4 of it where its tiles are cut. fp32 (32 steps a chunk): 64 x 128 1.03, 64 x 64 0.6, the same rate at the
-// matrix cores' limit (8192, 8, 1024, 4096: 526 us, 131 TFLOP/s, 64 x 64 571; 1501, 10, 2056,
-// 520: 77.6 and 74.0).
+// or 0.6 or 0.4 of it where its tiles are cut. fp32 (32 steps a chunk): 64 x 128 1.03,
+// 64 x 64 0.6, the same rate at the matrix cores' limit (8192, 8, 1024, 4096: 526 us,
+// 131 TFLOP/s, 64 x 64 571; 1501, 10, 2056, 520: 77.6 and 74.0).
 struct TileCost {
     int bm, bn;
     double alone, many;
@@ -1039,9 +1039,12 @@ template <class In, int kForm>
 hipError_t launch_form(const LinearCall &c, hipStream_t s) {
     const int64_t avg = c.N / c.E;
     if (c.parts > 1) {
-        if constexpr (kForm != kTN) return launch_tiles<In, kForm, 64, 64, 2, 2, 3, kInParts>(c, s);
-        else if constexpr (In::kBf16) return launch_tiles<In, kForm, 128, 128, 2, 2, 2, kInParts>(c, s);
-        else return launch_tiles<In, kForm, 64, 128, 2, 2, 2, kInParts>(c, s);
+        if constexpr (kForm != kTN)
+            return launch_tiles<In, kForm, 64, 64, 2, 2, 3, kInParts>(c, s);
+        else if constexpr (In::kBf16)
+            return launch_tiles<In, kForm, 128, 128, 2, 2, 2, kInParts>(c, s);
+        else
+            return launch_tiles<In, kForm, 64, 128, 2, 2, 2, kInParts>(c, s);
     }
     if constexpr (kForm == kTN) {
         // A tile stores its matrix's part once and multiplies little, so the tile matters
@@ -1061,7 +1064,8 @@ hipError_t launch_form(const LinearCall &c, hipStream_t s) {
         if (avg < 32) return launch_tiles<F32, kForm, 32, 128, 1, 4, 3, kEach>(c, s);
         const int64_t tiles =
             (c.N / 64 + c.E / 2) * (((kForm == kNT ? c.O : c.K) + 127) / 128);
-        if (tiles < 4 * kUnitsOfDevice) return launch_tiles<F32, kForm, 64, 64, 2, 2, 2, kEach>(c, s);
+        if (tiles < 4 * kUnitsOfDevice)
+            return launch_tiles<F32, kForm, 64, 64, 2, 2, 2, kEach>(c, s);
         return launch_tiles<F32, kForm, 64, 128, 2, 2, 2, kEach>(c, s);
     } else {
         // A few rows: the matrices' bytes count, and what keeps most of them in flight (64 rows

@@ -272,10 +272,10 @@ __global__ __launch_bounds__(kBlock<R>) void norm_backward_kernel(
 // four waves).
 template <int W>
 __global__ __launch_bounds__(64 * W) void norm_weights_kernel(const float *__restrict__ part,
-                                                           const int32_t *__restrict__ offsets,
-                                                           float *__restrict__ dg,
-                                                           float *__restrict__ db, int N, int d,
-                                                           int run) {
+                                                              const int32_t *__restrict__ offsets,
+                                                              float *__restrict__ dg,
+                                                              float *__restrict__ db, int N, int d,
+                                                              int run) {
     __shared__ float lds[W][64];
     const int e = blockIdx.y;
     const int lane = threadIdx.x & 63;

@@ -51,9 +51,6 @@ struct RowChunk {
     __device__ static void store(void *base, int64_t chunk, const float (&v)[kN]) {
         reinterpret_cast<u32x4_t *>(base)[chunk] = narrow(v);
     }
-    __device__ static void store_once(void *base, int64_t chunk, const float (&v)[kN]) {
-        __builtin_nontemporal_store(narrow(v), reinterpret_cast<u32x4_t *>(base) + chunk);
-    }
 };
 
 // Sum over the 64 lanes, in every lane: rows of 16 lanes turn by 8, 4, 2 and 1, then rows and
@@ -61,7 +58,8 @@ struct RowChunk {
 // LDS takes an order of magnitude longer).
 template <int kControl>
 __device__ inline float turned(float v) {
-    return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), kControl, 0xf, 0xf, true));
+    return __uint_as_float(
+        __builtin_amdgcn_update_dpp(0, __float_as_uint(v), kControl, 0xf, 0xf, true));
 }
 __device__ inline float wave_sum(float v) {
     typedef unsigned u32x2_t __attribute__((ext_vector_type(2)));
@@ -70,10 +68,12 @@ __device__ inline float wave_sum(float v) {
     v += turned<0x122>(v);
     v += turned<0x121>(v);
     const uint32_t a = __float_as_uint(v);
-    const u32x2_t r = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_permlane16_swap(a, a, false, false));
+    const u32x2_t r =
+        __builtin_bit_cast(u32x2_t, __builtin_amdgcn_permlane16_swap(a, a, false, false));
     v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
     const uint32_t b = __float_as_uint(v);
-    const u32x2_t h = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_permlane32_swap(b, b, false, false));
+    const u32x2_t h =
+        __builtin_bit_cast(u32x2_t, __builtin_amdgcn_permlane32_swap(b, b, false, false));
     return __uint_as_float(h[0]) + __uint_as_float(h[1]);
 }
 

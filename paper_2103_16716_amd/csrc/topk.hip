@@ -13,8 +13,6 @@
 //   pair_count_kernel   the same counts for choices that are given
 //   pair_scan_kernel    E > 512: per expert, the pairs in earlier blocks
 //   pair_place_kernel   offsets, perm and slots
-#include <mutex>
-
 #include "common.hpp"
 #include "internal.hpp"
 
@@ -224,8 +222,8 @@ __global__ __launch_bounds__(kChoosers<C>) void topk_count_kernel(
     for (int e = threadIdx.x; e <= E; e += kChoosers<C>) hist[e] = 0;
     __syncthreads();
     const int64_t t0 = blockIdx.x * tokens;
-    choose<kChoosers<C>, G, C, L>(S, t0, t0 + tokens < T ? t0 + tokens : T, E, k, assign, scores, hist,
-                    [](int64_t, int) {});
+    choose<kChoosers<C>, G, C, L>(S, t0, t0 + tokens < T ? t0 + tokens : T, E, k, assign, scores,
+                                  hist, [](int64_t, int) {});
     __syncthreads();
     for (int e = threadIdx.x; e <= E; e += kChoosers<C>)
         counts[(int64_t)blockIdx.x * (E + 1) + e] = hist[e];
@@ -418,7 +416,7 @@ __global__ __launch_bounds__(kThreads) void route_small_kernel(
     for (int e = threadIdx.x; e <= E; e += kThreads) lds[e] = 0;
     __syncthreads();
     choose<kThreads, G, C, L>(S, 0, T, E, k, assign, scores, lds,
-                    [&](int64_t p, int e) { of_pair[p] = (uint16_t)e; });
+                              [&](int64_t p, int e) { of_pair[p] = (uint16_t)e; });
     __syncthreads();
     place<kThreads / 64>(0, (int64_t)T * k, E, lds, nullptr, lds + E + 1, wave_sum,
                          [&](int64_t p) { return (int)of_pair[p]; }, perm, slots, offsets);

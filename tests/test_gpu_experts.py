@@ -365,6 +365,52 @@ def test_products_in_parts(N, E, K, O, dtype):
     near_product(dw[-1], dy.t().contiguous(), x, N, U)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("N,E,K,O", [(90, 1, 4096, 264), (150, 2, 520, 4104), (3000, 2, 136, 72),
+                                     (33, 40, 520, 64), (2500, 3, 520, 2056)])
+def test_products_in_place_captured_and_at_once(N, E, K, O, dtype):
+    """The bits of a plain call: with y in the residual's place and dx in relu_of's, in every
+    replay of a graph (a workspace of its own, other work between the replays), and by two
+    streams at once."""
+    r = rng_of(N, E, K, O, 2)
+    x, w, dy, res, u = (dev(rows(r, n, dtype)[1])
+                        for n in ((N, K), (E, O, K), (N, O), (N, O), (N, K)))
+    b = dev(rows(r, (E, O), dtype)[1])
+    off = dev(some_offsets(r, N, E, 0, N))
+
+    def run():
+        return (pb.expert_linear(x, w, off, bias=b, relu=True, residual=res),
+                pb.expert_linear_dx(dy, w, off, relu_of=u), *pb.expert_linear_dw(dy, x, off))
+
+    want = run()
+    a, c = res.clone(), u.clone()
+    assert pb.expert_linear(x, w, off, bias=b, relu=True, residual=a, out=a) is a
+    assert pb.expert_linear_dx(dy, w, off, relu_of=c, out=c) is c
+    assert torch.equal(a, want[0]) and torch.equal(c, want[1])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = run()
+    for _ in range(3):
+        for t in got:
+            t.fill_(float("nan"))
+        graph.replay()
+        again = run()
+        torch.cuda.synchronize()
+        for p, q, s in zip(want, got, again):
+            assert torch.equal(p, q) and torch.equal(p, s)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    out = []
+    for st in streams:
+        st.wait_stream(torch.cuda.current_stream())
+    for _ in range(4):
+        for st in streams:
+            with torch.cuda.stream(st):
+                out.append(run())
+    torch.cuda.synchronize()
+    for got in out:
+        assert all(torch.equal(p, q) for p, q in zip(want, got))
+
+
 def test_products_keep_infinities_and_nan_in_their_rows():
     """A row of NaN or infinities spoils its own results only, and the ReLU keeps a NaN."""
     r = rng_of(11)
