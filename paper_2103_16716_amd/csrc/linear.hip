@@ -998,15 +998,15 @@ int pick_tile(int64_t N, int64_t E, int64_t cols) {
 // 128 x 128, fp32 64 x 128), with the time of a chunk of a tile alone on a unit. In one piece
 // and in parts, us: y of 1 row x 8192 to 512 in 32 parts 40 and 14 (fp32 165 and 18), of
 // 512 x 4096 to 256 in 6 23 and 12 (80 and 23); dx of 150 x 6152 to 1032 in 7 72 and 21 (121
-// and 41); dW 200 x 64 of 5000 rows in 19 67 and 15 (in 32 188 and 20), fp32 216 x 1672 of 8606
-// rows, three experts, in 3 109 and 76. What the rule leaves whole: dx of 1 x 512 to 2048, 5.8,
-// in 2 parts 7.1.
+// and 41), of 1000 x 4096 to 512, two experts, in 5 41 and 18; dW 200 x 64 of 5000 rows in 19 67
+// and 15 (in 32 188 and 20), fp32 216 x 1672 of 8606 rows, three experts, in 3 109 and 76. What
+// the rule leaves whole: dx of 1 x 512 to 2048, 5.8, in 2 parts 7.1.
 int parts_of(int form, bool bf16, int64_t N, int64_t E, int64_t K, int64_t O) {
     const int64_t steps = kChunk / (bf16 ? 2 : 4);
     const int64_t experts = E < N ? E : N;
     const int64_t cols = form == kNT ? O : K;
     const int64_t bm = form == kTN && bf16 ? 128 : 64, bn = form == kTN ? 128 : 64;
-    const double us = form == kTN ? (bf16 ? 0.85 : 1.05) : (bf16 ? 0.36 : 0.6);
+    const double us = form == kTN ? (bf16 ? 0.85 : 1.05) : bf16 ? (form == kNN ? 0.64 : 0.36) : 0.6;
     const int64_t rows = form == kTN ? E * ((O + bm - 1) / bm) : N / bm + experts;
     const int64_t tiles = rows * ((cols + bn - 1) / bn);
     const int64_t chunks = ((form == kNT ? K : form == kNN ? O : N / experts) + steps - 1) / steps;
