@@ -30,13 +30,13 @@ typedef float f32x16_t __attribute__((ext_vector_type(16)));
 
 #define BASE_LDS __attribute__((address_space(3)))
 
-// Tile `tile` of the experts' rows in tiles of BM, expert after expert: its
-// expert, its first row and the end of the expert's rows. Asked by whole waves.
-struct RowTile {
-    int e, r0, r1;
+// Whose tile is number `tile` of the experts' rows in tiles of BM, expert after expert: the
+// expert, its rows [r0, r1), its first tile and the number of its tiles. Asked by whole waves.
+struct RowTiles {
+    int e, r0, r1, first, count;
 };
-__device__ inline bool find_row_tile(const int32_t *__restrict__ offsets, int E, int N, int BM,
-                                     int tile, RowTile &out) {
+__device__ inline bool find_row_tiles(const int32_t *__restrict__ offsets, int E, int N, int BM,
+                                      int tile, RowTiles &out) {
     const int lane = threadIdx.x & 63;
     int before = 0;
     for (int e0 = 0; e0 < E; e0 += 64) {
@@ -55,8 +55,9 @@ __device__ inline bool find_row_tile(const int32_t *__restrict__ offsets, int E,
             const int f = __ffsll((unsigned long long)past) - 1;
             out.e = e0 + f;
             out.r1 = __builtin_amdgcn_readlane(z, f);
-            out.r0 = __builtin_amdgcn_readlane(a, f) +
-                     (tile - before - __builtin_amdgcn_readlane(sum - n, f)) * BM;
+            out.r0 = __builtin_amdgcn_readlane(a, f);
+            out.first = before + __builtin_amdgcn_readlane(sum - n, f);
+            out.count = __builtin_amdgcn_readlane(n, f);
             return true;
         }
         before += __builtin_amdgcn_readlane(sum, 63);
@@ -78,6 +79,13 @@ struct Bf16 {
     __device__ static f32x16_t mma(unit_t a, unit_t b, f32x16_t c, int) {
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
     }
+    // The sum of a result row's elements: products with ones.
+    using sum_t = f32x16_t;
+    __device__ static void add(unit_t a, sum_t &sum) {
+        const __bf16 i = (__bf16)1.0f;
+        sum = mma(unit_t{i, i, i, i, i, i, i, i}, a, sum, 0);
+    }
+    __device__ static float total(const sum_t &sum) { return sum[0]; }
 };
 struct F32 {
     static constexpr bool kBf16 = false;
@@ -88,6 +96,10 @@ struct F32 {
     __device__ static f32x16_t mma(unit_t a, unit_t b, f32x16_t c, int i) {
         return __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], b[i], c, 0, 0, 0);
     }
+    // (Here the matrix cores are what is short.)
+    using sum_t = float;
+    __device__ static void add(unit_t a, sum_t &sum) { sum += (a[0] + a[1]) + (a[2] + a[3]); }
+    __device__ static float total(sum_t sum) { return sum + __shfl_xor(sum, 32); }
 };
 
 // Waits until at most N vector-memory operations of this wave are in flight (loads into
@@ -247,10 +259,11 @@ struct LinearCall {
     const void *A, *B, *bias, *extra;   // extra: the residual (kNT) or relu_of (kNN)
     const int32_t *offsets;
     void *out;
+    float *db;    // kTN: sums of the rows of A, or null
     int N, E, K, O, relu;
     int block0;   // the number of the launch's first block
     // The contraction in `parts`, part p by blocks [p per_part, (p + 1) per_part), whose results
-    // follow each other in `out`, part_size of them (fp32) each.
+    // follow each other in `out`, part_size of them (fp32) each, and so those of db.
     int parts, per_part;
     int64_t part_size;
 };
@@ -375,16 +388,23 @@ struct Tiles {
     // landed for this wave. The last quarter of a chunk is multiplied behind the barrier that
     // hands its stage over: its operands are in registers by then, and the next chunk's
     // first ones are read beside it. Behind the last barrier all stages are free.
-    template <int X>
-    __device__ void contract(f32x16_t (&acc)[X][TN]) const {
+    //
+    // db's sums are taken beside them by the tiles of the first columns: each wave adds up 32
+    // rows (a kernel of its own read dy again: dW 4464 x 168 of 29473 rows 195 us, 125 so).
+    template <int X, bool kSum>
+    __device__ void contract(f32x16_t (&acc)[X][TN], typename In::sum_t &sum) const {
+        static_assert(X <= WN || kForm != kTN, "a wave for each 32 rows");
 #pragma unroll
         for (int x = 0; x < X; ++x)
 #pragma unroll
             for (int j = 0; j < TN; ++j)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) acc[x][j][i] = 0.0f;
-        unit_t a[2][X], b[2][TN];
+        if (kSum) sum = typename In::sum_t{};
+        unit_t a[2][X], b[2][TN], s[2];
+        const int sum_tile = wm + WM * (wn < X ? wn : 0);
         auto fetch = [&](int set, const char *st, int ks) {
+            if (kSum) s[set] = StageA::read(st, sum_tile, ks);
 #pragma unroll
             for (int x = 0; x < X; ++x) a[set][x] = StageA::read(st, wm + WM * x, ks);
 #pragma unroll
@@ -400,6 +420,7 @@ struct Tiles {
                     for (int x = 0; x < X; ++x)
                         acc[x][j] = kByRow ? In::mma(a[set][x], b[set][j], acc[x][j], i)
                                            : In::mma(b[set][j], a[set][x], acc[x][j], i);
+            if (kSum) In::add(s[set], sum);
         };
         barrier();
         if (nk > 0) fetch(0, lds, 0);
@@ -589,7 +610,10 @@ struct Tiles {
         f32x16_t acc[X][TN];
         Added<X> added;
         added.load_bias(*this);
-        contract<X>(acc);
+        typename In::sum_t sum;
+        const bool sums = kForm == kTN && t.n0 == 0 && c.db != nullptr;
+        if (sums) contract<X, kForm == kTN>(acc, sum);
+        else contract<X, false>(acc, sum);
         added.load_extra(*this);
         asm volatile("" ::: "memory");
         const Tile done = t;
@@ -597,6 +621,11 @@ struct Tiles {
             set(*next);
             issue_first();
             asm volatile("" ::: "memory");
+        }
+        if (sums) {
+            const int m = done.m0 + 32 * (wm + WM * wn) + lane;
+            const float total = In::total(sum);
+            if (lane < 32 && wn < X && m < done.m_end) c.db[(int64_t)done.e * c.O + m] = total;
         }
         finish<X>(done, acc, added);
         if (next != nullptr) {
@@ -757,6 +786,7 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_kernel(LinearCall c) {
         part = block / c.per_part;
         block -= part * c.per_part;
         c.out = static_cast<float *>(c.out) + part * c.part_size;
+        if (kForm == kTN && c.db != nullptr) c.db += part * c.part_size;
     }
     G g(c, lds);
     Tile t;
@@ -765,10 +795,18 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_kernel(LinearCall c) {
         if (!matrix_tile<BM, BN>(c, block, t, more)) return;
     } else {
         const int nn = (g.cols + BN - 1) / BN;
-        RowTile rt;
+        RowTiles rt;
         const int k = tile_of_block(count_row_tiles(c.offsets, c.E, c.N, BM) * nn, block);
-        if (k < 0 || !find_row_tile(c.offsets, c.E, c.N, BM, k / nn, rt)) return;
-        t = Tile{rt.e, rt.r0, rt.r1, k % nn * BN, 0, kForm == kNT ? c.K : c.O};
+        if (k < 0 || !find_row_tiles(c.offsets, c.E, c.N, BM, k / nn, rt)) return;
+        // Strips read a matrix once for their rows; one that the L2 (4 MB) holds most of is read
+        // there, and its rows go by once. By strips and without, us: y of 347 x 2592 to 3496, two
+        // experts (18 MB) 22 and 28; dx of 512 x 2048 to 2048 (8 MB) 17.6 and 24.7; y of
+        // 5801 x 4488 to 544, 30 experts (5 MB) 93 and 80, of 4692 x 3384 to 200, five (1 MB) 32
+        // and 26.
+        int m = k / nn - rt.first, n = k % nn;
+        if ((int64_t)c.K * c.O * G::kSize > (6 << 20))
+            tile_in_strip<8>(k - rt.first * nn, rt.count, nn, m, n);
+        t = Tile{rt.e, rt.r0 + m * BM, rt.r1, n * BN, 0, kForm == kNT ? c.K : c.O};
     }
     if constexpr (kPartial) {   // whole chunks; the last parts may have none
         const int chunks = t.s1 > t.s0 ? (t.s1 - t.s0 - 1) / G::S + 1 : 0;
@@ -839,11 +877,12 @@ __global__ __launch_bounds__(256) void join_rows_kernel(LinearCall c, const floa
     }
 }
 
-// The same for sums that are the result: n of them, n % 4 == 0.
+// The same for dW, n results, and db behind it, m; both % 4 == 0.
 __global__ __launch_bounds__(256) void join_sums_kernel(const float *__restrict__ part, int parts,
-                                                        int64_t part_size, int64_t n,
-                                                        float *__restrict__ out) {
-    for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < n;
+                                                        int64_t part_size, int64_t n, int64_t m,
+                                                        float *__restrict__ dw,
+                                                        float *__restrict__ db) {
+    for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < n + m;
          i += (int64_t)gridDim.x * 1024) {
         float4 sum = *reinterpret_cast<const float4 *>(part + i);
 #pragma unroll 8
@@ -851,53 +890,7 @@ __global__ __launch_bounds__(256) void join_sums_kernel(const float *__restrict_
             const float4 x = *reinterpret_cast<const float4 *>(part + p * part_size + i);
             sum.x += x.x, sum.y += x.y, sum.z += x.z, sum.w += x.w;
         }
-        *reinterpret_cast<float4 *>(out + i) = sum;
-    }
-}
-
-// db_e: column sums of dy over each expert's rows. A block for 128 bytes of an expert's
-// columns: eight lanes take a row's eight chunks, 32 rows in turn over four waves; blockIdx.z
-// its part of the rows, for part_size results each.
-template <bool BF16>
-__global__ __launch_bounds__(256) void row_sums_kernel(const void *__restrict__ dy,
-                                                       const int32_t *__restrict__ offsets,
-                                                       float *__restrict__ db, int N, int O,
-                                                       int64_t part_size) {
-    using Ck = RowChunk<BF16>;
-    __shared__ float lds[32][8 * Ck::kN + 1];
-    const int e = blockIdx.y;
-    const int ncs = O / Ck::kN;
-    const int g = threadIdx.x / 8;
-    const int a0 = row_bound(offsets, e, N), z0 = row_bound(offsets, e + 1, N);
-    const int64_t per = z0 > a0 ? (z0 - a0 - 1) / (int)gridDim.z + 1 : 0;
-    const int64_t a = a0 + blockIdx.z * per;
-    const int64_t z = a + per < z0 ? a + per : z0;
-    db += blockIdx.z * part_size;
-    for (int c0 = blockIdx.x * 8; c0 < ncs; c0 += gridDim.x * 8) {
-        const int c = c0 + threadIdx.x % 8;
-        float s[Ck::kN];
-#pragma unroll
-        for (int q = 0; q < Ck::kN; ++q) s[q] = 0.0f;
-        if (c < ncs) {
-#pragma unroll 4
-            for (int64_t r = a + g; r < z; r += 32) {
-                float v[Ck::kN];
-                Ck::widen(Ck::fetch(dy, r * ncs + c), v);
-#pragma unroll
-                for (int q = 0; q < Ck::kN; ++q) s[q] += v[q];
-            }
-        }
-#pragma unroll
-        for (int q = 0; q < Ck::kN; ++q) lds[g][threadIdx.x % 8 * Ck::kN + q] = s[q];
-        __syncthreads();
-        const int i = threadIdx.x;
-        const int col = c0 * Ck::kN + i;
-        if (i < 8 * Ck::kN && col < O) {
-            float sum = 0.0f;
-            for (int r = 0; r < 32; ++r) sum += lds[r][i];
-            db[(int64_t)e * O + col] = sum;
-        }
-        __syncthreads();
+        *reinterpret_cast<float4 *>(i < n ? dw + i : db + (i - n)) = sum;
     }
 }
 
@@ -1026,15 +1019,6 @@ int parts_of(int form, bool bf16, int64_t N, int64_t E, int64_t K, int64_t O) {
     return best;
 }
 
-// Parts of the rows whose sums are db: blocks for the whole device, of 256 rows at least (two
-// parts of 128 rows cost 1.5 us more than one of 256).
-int sum_parts(bool bf16, int64_t N, int64_t E, int64_t O) {
-    const int64_t blocks = (O * (bf16 ? 2 : 4) + 127) / 128 * E;
-    int64_t parts = 2 * kUnitsOfDevice / blocks;
-    if (parts > N / E / 256) parts = N / E / 256;
-    return parts < 4 ? 1 : parts > 64 ? 64 : (int)parts;
-}
-
 template <class In, int kForm>
 hipError_t launch_form(const LinearCall &c, hipStream_t s) {
     const int64_t avg = c.N / c.E;
@@ -1094,8 +1078,12 @@ hipError_t launch_call(LinearCall c, void *workspace, hipStream_t s) {
     void *out = c.out;
     const float *part = static_cast<const float *>(workspace);
     const int64_t cols = kForm == kNT ? c.O : c.K;
-    c.part_size = (kForm == kTN ? (int64_t)c.E * c.O : (int64_t)c.N) * cols;
+    const int64_t size = (kForm == kTN ? (int64_t)c.E * c.O : (int64_t)c.N) * cols;
+    const int64_t with_db = c.db != nullptr ? (int64_t)c.E * c.O : 0;
+    float *db = c.db;
+    c.part_size = size + with_db;
     c.out = workspace;
+    if (db != nullptr) c.db = static_cast<float *>(workspace) + size;
     hipError_t err = launch_form<In, kForm>(c, s);
     if (err != hipSuccess) return err;
     c.out = out;
@@ -1103,8 +1091,8 @@ hipError_t launch_call(LinearCall c, void *workspace, hipStream_t s) {
     if constexpr (kForm == kTN) {
         const int64_t blocks = (c.part_size + 1023) / 1024;
         hipLaunchKernelGGL(join_sums_kernel, dim3((unsigned)(blocks < kMost ? blocks : kMost)),
-                           dim3(256), 0, s, part, c.parts, c.part_size, c.part_size,
-                           static_cast<float *>(out));
+                           dim3(256), 0, s, part, c.parts, c.part_size, size, with_db,
+                           static_cast<float *>(out), db);
     } else {
         const int64_t blocks = ((int64_t)c.N * ((cols + 511) / 512) + 3) / 4;
         hipLaunchKernelGGL((join_rows_kernel<In, kForm>),
@@ -1138,21 +1126,13 @@ LinearCall call_of(const void *A, const void *B, const void *bias, const void *e
     return c;
 }
 
-// fp32 sums of a call's parts: of the products, then (dW) those of db.
-int64_t part_sums(int form, bool bf16, int64_t N, int64_t E, int64_t K, int64_t O) {
-    const int64_t parts = parts_of(form, bf16, N, E, K, O);
-    return parts == 1 ? 0 : parts * (form == kNT ? N * O : form == kNN ? N * K : E * O * K);
-}
-
 }  // namespace
 
 size_t linear_workspace_size(int product, int64_t N, int64_t E, int64_t K, int64_t O, int bf16) {
-    int64_t n = part_sums(product, bf16 != 0, N, E, K, O);
-    if (product == kTN) {
-        const int64_t parts = sum_parts(bf16 != 0, N, E, O);
-        if (parts > 1) n += parts * E * O;
-    }
-    return ((size_t)n * 4 + 255) / 256 * 256;
+    const int64_t parts = parts_of(product, bf16 != 0, N, E, K, O);
+    if (parts == 1) return 0;
+    const int64_t n = product == kNT ? N * O : product == kNN ? N * K : E * O * (K + 1);
+    return ((size_t)(parts * n) * 4 + 255) / 256 * 256;
 }
 
 hipError_t launch_linear(const void *x, const void *w, const void *bias, const void *residual,
@@ -1172,24 +1152,9 @@ hipError_t launch_linear_dx(const void *dy, const void *w, const void *relu_of,
 hipError_t launch_linear_dw(const void *dy, const void *x, const int32_t *offsets, float *dw,
                             float *db, int64_t N, int64_t E, int64_t K, int64_t O, int bf16,
                             void *workspace, hipStream_t s) {
-    const hipError_t err = launch<kTN>(
-        call_of(dy, x, nullptr, nullptr, offsets, dw, N, E, K, O, 0), bf16, workspace, s);
-    if (err != hipSuccess || db == nullptr) return err;
-    const int parts = sum_parts(bf16 != 0, N, E, O);
-    float *sums = db;
-    if (parts > 1) sums = static_cast<float *>(workspace) + part_sums(kTN, bf16 != 0, N, E, K, O);
-    const int64_t blocks = (O * (bf16 ? 2 : 4) + 127) / 128;
-    const dim3 grid((unsigned)(blocks < 1024 ? blocks : 1024), (unsigned)E, (unsigned)parts);
-    if (bf16)
-        hipLaunchKernelGGL(row_sums_kernel<true>, grid, dim3(256), 0, s, dy, offsets, sums, (int)N,
-                           (int)O, E * O);
-    else
-        hipLaunchKernelGGL(row_sums_kernel<false>, grid, dim3(256), 0, s, dy, offsets, sums, (int)N,
-                           (int)O, E * O);
-    if (parts > 1)
-        hipLaunchKernelGGL(join_sums_kernel, dim3((unsigned)((E * O + 1023) / 1024)), dim3(256), 0,
-                           s, sums, parts, E * O, E * O, db);
-    return hipGetLastError();
+    LinearCall c = call_of(dy, x, nullptr, nullptr, offsets, dw, N, E, K, O, 0);
+    c.db = db;
+    return launch<kTN>(c, bf16, workspace, s);
 }
 
 }  // namespace base

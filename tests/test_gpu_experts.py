@@ -326,15 +326,15 @@ def test_products(N, E, K, O, dtype):
 
 
 # Few outputs and long sums: cut into parts (the number of them is in the comment, a product's
-# y, dx, dw and db in bf16 and fp32).
+# in bf16 and fp32).
 IN_PARTS = [(1, 1, 8192, 512),      # y 32, 32; one row, parts of four chunks
             (70, 1, 8192, 264),     # y 25, 25; uneven parts, columns behind 256
             (40, 3, 4104, 72),      # y 16, 32; a part of part of a chunk, the last ones empty
             (130, 1, 8, 4096),      # dx 16, 32
             (150, 2, 1032, 6152),   # dx 7, 7; three groups of columns in the join
             (300, 2, 8192, 136),    # y 14, 14; several tiles of rows
-            (5000, 3, 264, 40),     # dw 6, 13; db 6, 6
-            (5000, 1, 64, 200)]     # dw 19, 32; db 19, 19
+            (5000, 3, 264, 40),     # dw 6, 13
+            (5000, 1, 64, 200)]     # dw 19, 32
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
