@@ -262,9 +262,9 @@ struct LinearCall {
     float *db;    // kTN: sums of the rows of A, or null
     int N, E, K, O, relu;
     int block0;   // the number of the launch's first block
-    // The contraction in `parts`, part p by blocks [p per_part, (p + 1) per_part), whose results
-    // follow each other in `out`, part_size of them (fp32) each, and so those of db.
-    int parts, per_part;
+    // The contraction in `parts`, whose results follow each other in `out`, part_size of them
+    // (fp32) each, and so those of db.
+    int parts;
     int64_t part_size;
 };
 
@@ -783,8 +783,9 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_kernel(LinearCall c) {
     int block = c.block0 + (int)blockIdx.x;
     int part = 0;
     if constexpr (kPartial) {
-        part = block / c.per_part;
-        block -= part * c.per_part;
+        const int u = block >> 3;   // the parts of a tile on the same XCD, next to each other
+        part = u % c.parts;
+        block = u / c.parts * 8 + (block & 7);
         c.out = static_cast<float *>(c.out) + part * c.part_size;
         if (kForm == kTN && c.db != nullptr) c.db += part * c.part_size;
     }
@@ -927,7 +928,6 @@ hipError_t launch_tiles(const LinearCall &c, hipStream_t s) {
         if (kForm != kTN) blocks = nn * ((int64_t)c.N / BM + (c.E < c.N ? c.E : c.N));
         else blocks = nm * nn >= 32 ? (nm * nn + 7) / 8 * 8 * c.E : nm * nn * c.E;
         blocks = (blocks + 7) / 8 * 8;
-        call.per_part = (int)blocks;
         if (kHow == kInParts) blocks *= c.parts;
     }
     constexpr int64_t kMost = 1 << 22;   // a launch has fewer than 2^32 threads
@@ -950,23 +950,24 @@ hipError_t launch_tiles(const LinearCall &c, hipStream_t s) {
 //   128 x 128  0.85  0.62  (8192, 64, 1024, 4096: 155 us, 64 x 128 171, 64 x 64 202)
 //   64 x 128   0.62  0.4   (4096, 64, 1024, 4096: 127 us, 128 x 128 131, 32 x 64 182)
 //   64 x 64    0.36  0.27  (512, 1, 2048, 2048: 13.7 us, 64 x 128 22.7, 256 x 256 52)
-// The 256 x 256 tiles are one to a unit: a started round of them takes a whole one's time,
-// or 0.6 or 0.4 of it where its tiles are cut. fp32 (32 steps a chunk): 64 x 128 1.03,
+// Alone and by columns, 64 x 128 takes 0.8, 128 x 128 1.0, 64 x 64 0.64. The 256 x 256 tiles
+// are one to a unit: a started round of them takes a whole one's time, or 0.6 or 0.4 of it where
+// its tiles are cut. fp32 (32 steps a chunk): 64 x 128 1.03,
 // 64 x 64 0.6, the same rate at the matrix cores' limit (8192, 8, 1024, 4096: 526 us,
 // 131 TFLOP/s, 64 x 64 571; 1501, 10, 2056, 520: 77.6 and 74.0).
 struct TileCost {
     int bm, bn;
     double alone, many;
 };
-constexpr TileCost kCosts[] = {{64, 128, 0.62, 0.4}, {128, 128, 0.85, 0.62}, {256, 256, 1.6, 1.9},
-                               {64, 64, 0.36, 0.27}};
+constexpr TileCost kCosts[2][4] = {   // kNT, kNN
+    {{64, 128, 0.62, 0.4}, {128, 128, 0.85, 0.62}, {256, 256, 1.6, 1.9}, {64, 64, 0.36, 0.27}},
+    {{64, 128, 0.8, 0.4}, {128, 128, 1.0, 0.62}, {256, 256, 1.6, 1.9}, {64, 64, 0.64, 0.27}}};
 
-int pick_tile(int64_t N, int64_t E, int64_t cols) {
+int pick_tile(int form, int64_t N, int64_t E, int64_t cols, double &low) {
     const int64_t experts = E < N ? E : N;
     int best = 0;
-    double low = 0.0;
     for (int i = 0; i < 4; ++i) {
-        const TileCost &t = kCosts[i];
+        const TileCost &t = kCosts[form][i];
         // Half a tile goes to waste at an expert's end.
         double rows = (double)N / t.bm + 0.5 * experts;
         if (rows < experts) rows = (double)experts;
@@ -985,33 +986,42 @@ int pick_tile(int64_t N, int64_t E, int64_t cols) {
     return best;
 }
 
-// Parts of the contraction, for a call whose tiles do not fill the device once: of four chunks
-// at least, as many as bring the least time of whole rounds of tiles over the compute units
-// with the sums' way through memory and the launch that joins them. Tiles of 64 x 64 (kTN:
-// 128 x 128, fp32 64 x 128), with the time of a chunk of a tile alone on a unit. In one piece
-// and in parts, us: y of 1 row x 8192 to 512 in 32 parts 40 and 14 (fp32 165 and 18), of
-// 512 x 4096 to 256 in 6 23 and 12 (80 and 23); dx of 150 x 6152 to 1032 in 7 72 and 21 (121
-// and 41), of 1000 x 4096 to 512, two experts, in 5 41 and 18; dW 200 x 64 of 5000 rows in 19 67
-// and 15 (in 32 188 and 20), fp32 216 x 1672 of 8606 rows, three experts, in 3 109 and 76. What
-// the rule leaves whole: dx of 1 x 512 to 2048, 5.8, in 2 parts 7.1.
+// Parts of the contraction, for a call whose tiles leave compute units idle or with one tile
+// each, which a unit does not overlap with anything: the number with the least time of the
+// products (a chunk of a tile alone on a unit, and of each of several; tiles of 64 x 64, kTN
+// 128 x 128 or fp32 64 x 128), of the sums' way through memory and of the launch that joins
+// them, with four chunks at least in a part. In one piece and in parts, us: y of 1 row x 8192 to
+// 512 in 32 parts 40 and 14 (fp32 165 and 18), of 512 x 4096 to 256 in 6 23 and 12 (80 and 23);
+// dx of 150 x 6152 to 1032 72 and 21 (121 and 41), of 1000 x 4096 to 512, two experts, 41 and 18;
+// dW 200 x 64 of 5000 rows in 19 67 and 15 (in 32 188 and 20), fp32 216 x 1672 of 8606 rows, three
+// experts, in 3 109 and 76; fp32 dx of 3584 x 6112 to 344, seven experts, 204 and 158. What the
+// rule leaves whole: dx of 1 x 512 to 2048, 5.8, in 2 parts 7.1; and experts of few rows in many
+// tiles, which are bound by their matrices' bytes (fp32 y of 94 x 6976 to 1032, 27 experts, 158,
+// in parts 219).
 int parts_of(int form, bool bf16, int64_t N, int64_t E, int64_t K, int64_t O) {
     const int64_t steps = kChunk / (bf16 ? 2 : 4);
     const int64_t experts = E < N ? E : N;
     const int64_t cols = form == kNT ? O : K;
-    const int64_t bm = form == kTN && bf16 ? 128 : 64, bn = form == kTN ? 128 : 64;
-    const double us = form == kTN ? (bf16 ? 0.85 : 1.05) : bf16 ? (form == kNN ? 0.64 : 0.36) : 0.6;
-    const int64_t rows = form == kTN ? E * ((O + bm - 1) / bm) : N / bm + experts;
-    const int64_t tiles = rows * ((cols + bn - 1) / bn);
+    constexpr TileCost kPart[3][2] = {{{64, 64, 0.6, 0.48}, {64, 64, 0.36, 0.3}},
+                                      {{64, 64, 0.6, 0.48}, {64, 64, 0.64, 0.4}},
+                                      {{64, 128, 1.05, 0.9}, {128, 128, 0.85, 0.62}}};
+    const TileCost &t = kPart[form][bf16];
+    const int64_t rows = form == kTN ? E * ((O + t.bm - 1) / t.bm)
+                                     : (N + t.bm - 1) / t.bm + experts - 1;   // at most
+    const int64_t tiles = rows * ((cols + t.bn - 1) / t.bn);
+    if (tiles > (form != kTN && N / E < 32 ? 1 : 2) * kUnitsOfDevice) return 1;
     const int64_t chunks = ((form == kNT ? K : form == kNN ? O : N / experts) + steps - 1) / steps;
-    if (tiles > kUnitsOfDevice) return 1;
     const double results = form == kTN ? (double)E * O * K : (double)N * cols;
     const int64_t most = chunks / 4 < 32 ? chunks / 4 : 32;
     int best = 1;
-    double low = chunks * us;
-    for (int64_t p = 2; p <= most; ++p) {
-        const int64_t rounds = (tiles * p + kUnitsOfDevice - 1) / kUnitsOfDevice;
-        const double cost = rounds * chunks * us / p + 1.3 * (4.0 + 8.0 * p * results / 4e6);
-        if (cost < low) {
+    double low = 0.0, whole = 1e30;
+    if (bf16 && form != kTN) pick_tile(form, N, E, cols, whole);
+    for (int64_t p = 1; p <= most; ++p) {
+        const double many = t.many * ((tiles * p + kUnitsOfDevice - 1) / kUnitsOfDevice);
+        double cost = chunks * (many > t.alone ? many : t.alone) / p;
+        if (p == 1 && cost > chunks * whole) cost = chunks * whole;
+        if (p > 1) cost += 1.3 * (4.0 + 8.0 * p * results / 4e6);
+        if (p == 1 || cost < low) {
             best = (int)p;
             low = cost;
         }
@@ -1061,7 +1071,8 @@ hipError_t launch_form(const LinearCall &c, hipStream_t s) {
         if constexpr (kForm == kNN)
             if (avg <= 2)
                 return launch_tiles<Bf16, kForm, 32, 64, 1, 2, 2, kEach>(c, s);
-        switch (pick_tile(c.N, c.E, kForm == kNT ? c.O : c.K)) {
+        double cost;
+        switch (pick_tile(kForm, c.N, c.E, kForm == kNT ? c.O : c.K, cost)) {
             case 0: return launch_tiles<Bf16, kForm, 64, 128, 2, 2, 2, kEach>(c, s);
             case 1: return launch_tiles<Bf16, kForm, 128, 128, 2, 2, 2, kEach>(c, s);
             case 2: return launch_tiles<Bf16, kForm, 256, 256, 2, 4, 2, kWide>(c, s);
