@@ -952,9 +952,9 @@ hipError_t launch_tiles(const LinearCall &c, hipStream_t s) {
 //   64 x 64    0.36  0.27  (512, 1, 2048, 2048: 13.7 us, 64 x 128 22.7, 256 x 256 52)
 // Alone and by columns, 64 x 128 takes 0.8, 128 x 128 1.0, 64 x 64 0.64. The 256 x 256 tiles
 // are one to a unit: a started round of them takes a whole one's time, or 0.6 or 0.4 of it where
-// its tiles are cut. fp32 (32 steps a chunk): 64 x 128 1.03,
-// 64 x 64 0.6, the same rate at the matrix cores' limit (8192, 8, 1024, 4096: 526 us,
-// 131 TFLOP/s, 64 x 64 571; 1501, 10, 2056, 520: 77.6 and 74.0).
+// its tiles are cut. fp32 (32 steps a chunk): 64 x 128 1.03, 64 x 64 0.6, the same rate at the
+// matrix cores' limit (8192, 8, 1024, 4096: 526 us, 131 TFLOP/s, 64 x 64 571; 1501, 10, 2056,
+// 520, in one piece: 77.6 and 74.0).
 struct TileCost {
     int bm, bn;
     double alone, many;
@@ -1042,13 +1042,14 @@ hipError_t launch_form(const LinearCall &c, hipStream_t s) {
     }
     if constexpr (kForm == kTN) {
         // A tile stores its matrix's part once and multiplies little, so the tile matters
-        // for experts with many rows only (64 experts, 4096 x 1024: 64 rows of 128 x 128 and
-        // 256 x 256 tiles 212 and 229 us, 8192 rows 367 and 357, 16384 rows 498 and 478).
+        // for experts with many rows only (128 x 128 and 256 x 256 tiles, us: 64 experts of
+        // 4096 x 1024 with 16 rows each 219 and 247, 128 rows 317 and 312, 256 rows 428 and 366;
+        // eight of 8192 x 2048 with 128 rows each 133 and 148, 256 rows 181 and 174).
         if constexpr (!In::kBf16) {
             return launch_tiles<F32, kTN, 64, 128, 2, 2, 2, kEach>(c, s);
         } else {
             const int64_t tiles = (int64_t)c.E * ((c.O + 255) / 256) * ((c.K + 255) / 256);
-            if (avg >= 96 && tiles >= 192)
+            if (avg >= 160 && tiles >= 192)
                 return launch_tiles<Bf16, kTN, 256, 256, 2, 4, 2, kWide>(c, s);
             return launch_tiles<Bf16, kTN, 128, 128, 2, 2, 2, kEach>(c, s);
         }
