@@ -132,15 +132,18 @@ __global__ __launch_bounds__(kBlock<R>) void norm_kernel(
 template <int R>
 constexpr int kRun = 16 * (kBlock<R> / R);
 
+// (Two waves a SIMD, which the compiler else misses by a few registers, and the groups' sums
+// by four columns of a lane, without bank conflicts: 32768 rows of 2048 in bf16 91 us, 87 so;
+// with one wave 104.)
 template <bool BF16, int R, int C>
-__global__ __launch_bounds__(kBlock<R>) void norm_backward_kernel(
+__global__ __launch_bounds__(kBlock<R>, 2) void norm_backward_kernel(
     const void *dy, const void *__restrict__ x, const void *__restrict__ g,
     const float *__restrict__ mean, const float *__restrict__ rstd, const void *residual,
     RowMap map, void *dx, float *__restrict__ part, int d) {
     using Ck = RowChunk<BF16>;
     constexpr int kN = Ck::kN;
     constexpr int kGroups = kBlock<R> / R;
-    extern __shared__ float sums[];   // [2 d], more than one group only
+    extern __shared__ float sums[];   // [2][C kN / 4][R][4], more than one group only
     __shared__ float lds[16];
     const int ncs = d / kN;
     const int l = threadIdx.x % R;
@@ -237,14 +240,14 @@ __global__ __launch_bounds__(kBlock<R>) void norm_backward_kernel(
                             if (l + c * R < ncs)
 #pragma unroll
                                 for (int q = 0; q < kN; ++q) {
-                                    const int i = (l + c * R) * kN + q;
+                                    const int i = ((c * kN + q) / 4 * R + l) * 4 + q % 4;
                                     if (w0 > 0) {
                                         dg[c][q] += sums[i];
-                                        db[c][q] += sums[d + i];
+                                        db[c][q] += sums[C * kN * R + i];
                                     }
                                     if (w0 < kGroups - 1) {
                                         sums[i] = dg[c][q];
-                                        sums[d + i] = db[c][q];
+                                        sums[C * kN * R + i] = db[c][q];
                                     }
                                 }
                     __syncthreads();
@@ -328,8 +331,8 @@ void launch_norm_as(const NormCall &n, hipStream_t s) {
         return;
     }
     hipLaunchKernelGGL((norm_backward_kernel<BF16, R, C>), dim3((unsigned)blocks),
-                       dim3(kBlock<R>), kGroups > 1 ? (size_t)n.d * 8 : 0, s, n.dy, n.x, n.g,
-                       n.mean_in, n.rstd_in, n.residual, n.map, n.y, n.part, n.d);
+                       dim3(kBlock<R>), kGroups > 1 ? C * RowChunk<BF16>::kN * R * 8 : 0, s, n.dy,
+                       n.x, n.g, n.mean_in, n.rstd_in, n.residual, n.map, n.y, n.part, n.d);
 }
 
 // Threads per row: a wave up to 4 chunks a lane, then a block of four waves, then of eight
