@@ -944,24 +944,25 @@ hipError_t launch_tiles(const LinearCall &c, hipStream_t s) {
 
 // The choice of tile. The row ranges are on the GPU, so it goes by the rows an expert has
 // on average. A product takes the larger of one tile's time and the time of all tiles over
-// the compute units; measured us per chunk of a tile alone on a unit, and of a tile among
-// many (bf16, 64 steps a chunk; calls of N rows, E experts, K inputs, O outputs in brackets):
-//   256 x 256  1.6   1.9   (16384, 64, 1024, 4096: 215 us, 128 x 128 243, 64 x 128 311)
-//   128 x 128  0.85  0.62  (8192, 64, 1024, 4096: 155 us, 64 x 128 171, 64 x 64 202)
-//   64 x 128   0.62  0.4   (4096, 64, 1024, 4096: 127 us, 128 x 128 131, 32 x 64 182)
-//   64 x 64    0.36  0.27  (512, 1, 2048, 2048: 13.7 us, 64 x 128 22.7, 256 x 256 52)
-// Alone and by columns, 64 x 128 takes 0.8, 128 x 128 1.0, 64 x 64 0.64. The 256 x 256 tiles
-// are one to a unit: a started round of them takes a whole one's time, or 0.6 or 0.4 of it where
-// its tiles are cut. fp32 (32 steps a chunk): 64 x 128 1.03, 64 x 64 0.6, the same rate at the
-// matrix cores' limit (8192, 8, 1024, 4096: 526 us, 131 TFLOP/s, 64 x 64 571; 1501, 10, 2056,
-// 520, in one piece: 77.6 and 74.0).
+// the compute units: us per chunk of a tile alone on a unit, and of a tile among many (bf16,
+// 64 steps a chunk). The numbers are measured ones, set within their spread so that the choices
+// are best over 400 calls of all sizes: those take 1.9 % longer than with the best tile each.
+// For instance (N rows, E experts, K inputs, O outputs; us):
+//   256 x 256  13140, 3, 7256, 1872: 402, 128 x 128 520, 64 x 128 648
+//   128 x 128  8192, 64, 1024, 4096: 155, 64 x 128 171, 64 x 64 202
+//   64 x 128   314, 20, 2960, 4864: 125, 128 x 128 144, 64 x 64 132
+//   64 x 64    512, 1, 2048, 2048: 13.7, 64 x 128 22.7, 256 x 256 52
+// The 256 x 256 tiles are one to a unit: a started round of them takes a whole one's time, or
+// 0.9 or 0.45 of it where its tiles are cut. fp32 (32 steps a chunk): 64 x 128 1.03, 64 x 64
+// 0.6, the same rate at the matrix cores' limit (8192, 8, 1024, 4096: 526 us, 131 TFLOP/s,
+// 64 x 64 571; 1501, 10, 2056, 520, in one piece: 77.6 and 74.0).
 struct TileCost {
     int bm, bn;
     double alone, many;
 };
 constexpr TileCost kCosts[2][4] = {   // kNT, kNN
-    {{64, 128, 0.62, 0.4}, {128, 128, 0.85, 0.62}, {256, 256, 1.6, 1.9}, {64, 64, 0.36, 0.27}},
-    {{64, 128, 0.8, 0.4}, {128, 128, 1.0, 0.62}, {256, 256, 1.6, 1.9}, {64, 64, 0.64, 0.27}}};
+    {{64, 128, 0.65, 0.45}, {128, 128, 0.85, 0.68}, {256, 256, 1.7, 1.85}, {64, 64, 0.37, 0.27}},
+    {{64, 128, 0.8, 0.4}, {128, 128, 1.05, 0.62}, {256, 256, 1.6, 1.7}, {64, 64, 0.64, 0.28}}};
 
 int pick_tile(int form, int64_t N, int64_t E, int64_t cols, double &low) {
     const int64_t experts = E < N ? E : N;
@@ -973,9 +974,10 @@ int pick_tile(int form, int64_t N, int64_t E, int64_t cols, double &low) {
         if (rows < experts) rows = (double)experts;
         double rounds = rows * ((cols + t.bn - 1) / t.bn) / kUnitsOfDevice;
         if (t.bm == 256) {
+            rounds *= 1.03;   // (a few tiles more than on average start another round)
             const double whole = (double)(int64_t)rounds;
             const double rest = rounds - whole;
-            rounds = whole + (rest > 0.5 ? 1.0 : rest > 0.25 ? 0.6 : rest > 0.0 ? 0.4 : 0.0);
+            rounds = whole + (rest > 0.5 ? 1.0 : rest > 0.25 ? 0.9 : rest > 0.0 ? 0.45 : 0.0);
         }
         const double cost = rounds * t.many > t.alone ? rounds * t.many : t.alone;
         if (i == 0 || cost < low) {

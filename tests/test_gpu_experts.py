@@ -366,6 +366,36 @@ def test_products_in_parts(N, E, K, O, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("N,E,K,O", [(7, 3, 16, 24), (90, 1, 4096, 264), (150, 2, 520, 4104),
+                                     (3000, 2, 136, 72), (2500, 3, 520, 2056)])
+def test_a_batch_of_padding(N, E, K, O, dtype):
+    """No token has an expert: the router says so, results and gradients by the rows stay as
+    they were, those by the weights are zero."""
+    t = torch.bfloat16 if dtype == "bf16" else torch.float32
+    route = pb.topk_assign(torch.full((N, E), -float("inf"), device="cuda"), 1)
+    assert bool((route.assign == -1).all()) and bool((route.slots == -1).all())
+    assert bool((route.perm == -1).all()) and bool((route.offsets == 0).all())
+    off = route.offsets
+    x, dy = (torch.full((N, n), float("nan"), dtype=t, device="cuda") for n in (K, O))
+    w = torch.randn(E, O, K, device="cuda").to(t)
+    y, dx = torch.full_like(dy, 7.0), torch.full_like(x, 7.0)
+    pb.expert_linear(x, w, off, out=y)
+    pb.expert_linear_dx(dy, w, off, out=dx)
+    dw, db = pb.expert_linear_dw(dy, x, off)
+    _, mean, rstd = pb.expert_norm(x, w[:, 0].contiguous(), None, off, out=dx)
+    dg, dbias = pb.expert_norm_backward(x, x, w[:, 0].contiguous(), mean, rstd, off, out=dx)[1:]
+    assert bool((y == 7).all()) and bool((dx == 7).all())
+    for z in (dw, db, dg, dbias):
+        assert bool((z == 0).all())
+    h = torch.randn(N, K, device="cuda").to(t)
+    assert torch.equal(pb.combine(x, route.slots, residual=h), h)
+    w1 = torch.full((N, 1), float("nan"), device="cuda")
+    assert torch.equal(pb.combine(x, route.slots, weights=w1, residual=h), h)
+    dF, dwt = pb.combine_backward(h, x, route.slots, w1, out=torch.full_like(x, 7.0))
+    assert bool((dF == 7).all()) and bool((dwt == 0).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("N,E,K,O", [(90, 1, 4096, 264), (150, 2, 520, 4104), (3000, 2, 136, 72),
                                      (33, 40, 520, 64), (2500, 3, 520, 2056)])
 def test_products_in_place_captured_and_at_once(N, E, K, O, dtype):
