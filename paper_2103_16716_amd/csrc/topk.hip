@@ -97,11 +97,11 @@ __device__ inline void merge_from(double (&a)[L]) {
     merge_lists(a, b);
 }
 
-// The L best of a row of E <= 4 G C scores, in every one of the G lanes (16 or 64) that
-// share it: each lane sorts its own, four consecutive experts per step of 4 G, then lists
-// are merged with those of lanes further round (a row of 16 lanes turns by 8, 4, 2, 1).
+// The L best of a lane's share of a row of E <= 4 G C scores: four consecutive experts per
+// step of 4 G.
 template <int G, int C, int L>
-__device__ inline void best_of_row(const float *__restrict__ row, int E, int g, double (&best)[L]) {
+__device__ inline void best_of_lane(const float *__restrict__ row, int E, int g,
+                                    double (&best)[L]) {
     constexpr int V = 4 * C;
     float v[V];
 #pragma unroll
@@ -134,6 +134,13 @@ __device__ inline void best_of_row(const float *__restrict__ row, int E, int g, 
             merge_lists(best, more);
         }
     }
+}
+
+// The L best of a row, in every one of the G lanes (16 or 64) that share it: lists are merged
+// with those of lanes further round (a row of 16 lanes turns by 8, 4, 2, 1).
+template <int G, int C, int L>
+__device__ inline void best_of_row(const float *__restrict__ row, int E, int g, double (&best)[L]) {
+    best_of_lane<G, C, L>(row, E, g, best);
     merge_from<0x128>(best);
     merge_from<0x124>(best);
     merge_from<0x122>(best);
@@ -147,6 +154,28 @@ __device__ inline void best_of_row(const float *__restrict__ row, int E, int g, 
             merge_lists(best, b);
         }
     }
+}
+
+// The same of two rows by 16 lanes, the first's in the lower eight and the second's in the
+// upper: half as many merges a row, which in this order (8 round, the mirror of eight, 2, 1)
+// meet all eight lanes. 131072 tokens, 8 of 64: 37.9 us one at a time, 31.6; 65536, 8 of 256:
+// 38.6 and 36.1.
+template <int C, int L>
+__device__ inline void best_of_two_rows(const float *__restrict__ row, const float *__restrict__ row2,
+                                        int E, int g, double (&best)[L]) {
+    double other[L];
+    best_of_lane<16, C, L>(row, E, g, best);
+    best_of_lane<16, C, L>(row2, E, g, other);
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+        const double give = g < 8 ? other[i] : best[i];
+        best[i] = g < 8 ? best[i] : other[i];
+        other[i] = move_in_row<0x128>(give);
+    }
+    merge_lists(best, other);
+    merge_from<0x141>(best);
+    merge_from<0x4e>(best);
+    merge_from<0xb1>(best);
 }
 
 // More choices than the lists hold: k rounds, each of which takes the best of the row and
@@ -182,18 +211,36 @@ __device__ inline void choose(const float *__restrict__ S, int64_t t0, int64_t t
                               int32_t *__restrict__ assign, float *__restrict__ scores,
                               int32_t *hist, Keep keep) {
     const int g = threadIdx.x % G;
+    const auto emit_of = [&](int64_t t, int j, double key) {
+        const uint32_t ord = key_ord(key);
+        const int a = ord != 0 ? key_expert(key) : -1;
+        assign[t * k + j] = a;
+        if (scores != nullptr) scores[t * k + j] = ord != 0 ? f32_unord(ord) : -INFINITY;
+        if (hist != nullptr) atomicAdd(&hist[a >= 0 ? a : E], 1);
+        keep(t * k + j, a >= 0 ? a : E);
+    };
+    if constexpr (G == 16 && L == 8) {
+        if (t1 - t0 > kT / G) {   // more than one round of the block: two tokens at a time
+            for (int64_t tb = t0; tb < t1; tb += kT / G * 2) {
+                const int64_t t = tb + threadIdx.x / G * 2;
+                const int64_t mine = t + (g >> 3);
+                double best[L];
+                best_of_two_rows<C, L>(S + (t < t1 ? t : t0) * E, S + (t + 1 < t1 ? t + 1 : t0) * E,
+                                       E, g, best);
+                double key = best[0];
+#pragma unroll
+                for (int i = 1; i < L; ++i)
+                    if ((g & 7) == i) key = best[i];
+                if (mine < t1 && (g & 7) < k) emit_of(mine, g & 7, key);
+            }
+            return;
+        }
+    }
     for (int64_t tb = t0; tb < t1; tb += kT / G) {
         const int64_t t = tb + threadIdx.x / G;
         const bool live = t < t1;
         const float *row = S + (live ? t : t0) * E;
-        const auto emit = [&](int j, double key) {
-            const uint32_t ord = key_ord(key);
-            const int a = ord != 0 ? key_expert(key) : -1;
-            assign[t * k + j] = a;
-            if (scores != nullptr) scores[t * k + j] = ord != 0 ? f32_unord(ord) : -INFINITY;
-            if (hist != nullptr) atomicAdd(&hist[a >= 0 ? a : E], 1);
-            keep(t * k + j, a >= 0 ? a : E);
-        };
+        const auto emit = [&](int j, double key) { emit_of(t, j, key); };
         if constexpr (L > 0) {
             double best[L];
             best_of_row<G, C, L>(row, E, g, best);
@@ -399,8 +446,8 @@ __global__ __launch_bounds__(64 * kWaves) void pair_place_kernel(
 
 // Few tokens: the latency of launches is what counts, so one block does it all and keeps the
 // pairs' experts in LDS. us in a graph, one block and two launches: 64 tokens, 2 of 64 experts
-// 4.5 and 10; 256 tokens 7.6 and 10.1; 128 tokens, 8 of 256 13.0 and 15; 256 tokens 23.2 and
-// 15.5, so by the scores as well.
+// 4.5 and 10; 256 tokens 7.6 and 10.1; 128 tokens, 8 of 256 11.5 and 15; 256 tokens 19.9 and
+// 16.7, so by the scores as well.
 constexpr int kSmallTokens = 256;
 constexpr int kSmallPairs = 2048;
 constexpr int kSmallScores = 32768;

@@ -59,7 +59,9 @@ def some_offsets(rng, N, E, first=0, last=None):
 
 @pytest.mark.parametrize("T,E,k", [(1, 1, 1), (1, 8, 8), (5, 3, 2), (48, 64, 2), (300, 100, 7),
                                    (1000, 128, 2), (2049, 256, 8), (513, 257, 3), (777, 512, 4),
-                                   (130, 1021, 5), (64, 2048, 64), (70000, 16, 2), (4097, 6, 6)])
+                                   (130, 1021, 5), (64, 2048, 64), (70000, 16, 2), (4097, 6, 6),
+                                   (65, 40, 3), (255, 128, 8), (255, 100, 4), (20001, 256, 8),
+                                   (17000, 90, 5), (16385, 200, 3), (33000, 60, 8)])
 def test_topk_assign(T, E, k):
     r = rng_of(T, E, k)
     S = r.standard_normal((T, E), dtype=np.float32)
