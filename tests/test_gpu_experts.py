@@ -5,6 +5,8 @@ Bounds: a fp32 sum of n terms in any order is off by at most n u sum |terms|, u 
 2^-24 (products of bf16 are exact, a fp32 product adds one more u); a result stored
 in bf16 is off by at most 2^-8 of its value more (half a step). Each test adds up the
 roundings its formula makes. Integers are equal."""
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -685,6 +687,30 @@ def test_layer_captured_and_replayed(dtype):
         assert 0 < routed < 400
         for n in want:
             assert torch.equal(got[n], want[n]), n
+
+
+def test_layer_from_two_threads():
+    """Threads with streams of their own: the library keeps nothing between calls."""
+    H, S, p, dOut = block_inputs(T=700, E=8, d=256, inner=1024)
+    H, S, dOut, p = dev(H), dev(S), dev(dOut), {n: dev(v) for n, v in p.items()}
+    want = block(H, S, 2, p, dOut)
+    torch.cuda.synchronize()
+    wrong, done = [], []
+
+    def work():
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(6):
+                got = block(H, S, 2, p, dOut)
+                torch.cuda.current_stream().synchronize()
+                wrong.extend(n for n in want if not torch.equal(got[n], want[n]))
+        done.append(1)
+
+    threads = [threading.Thread(target=work) for _ in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert len(done) == 2 and not wrong
 
 
 def test_layer_on_a_stream_of_its_own():
