@@ -1047,16 +1047,16 @@ hipError_t launch_form(const LinearCall &c, hipStream_t s) {
         // experts with many rows only (128 x 128 and 256 x 256 tiles, us: 64 experts of
         // 4096 x 1024 with 16 rows each 219 and 247, 128 rows 317 and 312, 256 rows 428 and 366;
         // eight of 8192 x 2048 with 128 rows each 133 and 148, 256 rows 181 and 174), where its
-        // started rounds take less time than all smaller tiles (a chunk of one 1.95 and, among
+        // started rounds take less time than all smaller tiles (a chunk of one 1.9 and, among
         // others, 0.58; three experts of 5384 x 520, 27587 rows, 261 and 353, 43 of 264 x 1696,
-        // 7447 rows, 30 and 53).
+        // 7447 rows, 30 and 53; over 280 calls 1.2 % longer than with the better tile each).
         if constexpr (!In::kBf16) {
             return launch_tiles<F32, kTN, 64, 128, 2, 2, 2, kEach>(c, s);
         } else {
             const int64_t wide = (int64_t)c.E * ((c.O + 255) / 256) * ((c.K + 255) / 256);
             const int64_t tiles = (int64_t)c.E * ((c.O + 127) / 128) * ((c.K + 127) / 128);
             const double rounds = (double)((wide + kUnitsOfDevice - 1) / kUnitsOfDevice);
-            if (avg >= 160 && rounds * 1.95 < (double)tiles / kUnitsOfDevice * 0.58)
+            if (avg >= 160 && rounds * 1.9 < (double)tiles / kUnitsOfDevice * 0.58)
                 return launch_tiles<Bf16, kTN, 256, 256, 2, 4, 2, kWide>(c, s);
             return launch_tiles<Bf16, kTN, 128, 128, 2, 2, 2, kEach>(c, s);
         }
