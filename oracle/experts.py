@@ -146,3 +146,53 @@ def linear_dw(dy, x, e, E):
         dw[i] = dy[r].T @ x[r]
         db[i] = dy[r].sum(axis=0)
     return dw, db
+
+
+def routed_weights(v):
+    """Softmax over a token's chosen scores v [T, k]; 0 for a choice of score -inf."""
+    v = np.asarray(v, dtype=np.float64)
+    top = v.max(axis=1, keepdims=True)
+    w = np.exp(v - np.where(top > -np.inf, top, 0.0))
+    return w / np.maximum(w.sum(axis=1, keepdims=True), 1e-300)
+
+
+def layer(H, S, k, p, eps):
+    """A layer of such experts, p their parameters g, b, W1, b1, W2, b2:
+        out[t] = H[t] + sum_j w[t, j] f_e(H[t]),  e = assign[t, j],
+        f_e(h) = W2_e max(W1_e norm_e(h) + b1_e, 0) + b2_e,  w[t] = softmax(scores[t]).
+    Every intermediate result, those on routed rows for the n rows there are."""
+    H = np.asarray(H, dtype=np.float64)
+    assign, scores = topk(S, k)
+    perm, slots, offsets = sort_pairs(assign, np.asarray(S).shape[1])
+    n = offsets[-1]
+    e, token = row_experts(offsets, n), perm[:n] // k
+    w = routed_weights(scores)
+    y, mean, rstd = norm(H[token], p["g"], p["b"], e, eps)
+    z = linear(y, p["W1"], p["b1"], e)
+    u = np.maximum(z, 0.0)
+    f = linear(u, p["W2"], p["b2"], e)
+    return dict(assign=assign, slots=slots, e=e, token=token, w=w, y=y, mean=mean, rstd=rstd, z=z,
+                u=u, f=f, out=combine(f, slots, w, H))
+
+
+def layer_backward(H, S, k, p, dOut, eps):
+    """(layer's results, the gradients of <out, dOut> by H, S, w, each parameter and each
+    intermediate result, named d and it)."""
+    H, dOut = np.asarray(H, dtype=np.float64), np.asarray(dOut, dtype=np.float64)
+    c = layer(H, S, k, p, eps)
+    e, token, E = c["e"], c["token"], np.asarray(S).shape[1]
+    df, dw = combine_backward(dOut, c["f"], c["slots"], c["w"], np.zeros((len(token), H.shape[1])))
+    dW2, db2 = linear_dw(df, c["u"], e, E)
+    dz = linear_dx(df, p["W2"], e, relu_of=c["u"])
+    dW1, db1 = linear_dw(dz, c["y"], e, E)
+    dy = linear_dx(dz, p["W1"], e)
+    dx, dg, db = norm_backward(dy, H[token], p["g"], e, eps)
+    dH = dOut.copy()
+    np.add.at(dH, token, dx)
+    dv = c["w"] * (dw - (c["w"] * dw).sum(axis=1, keepdims=True))
+    dS = np.zeros(np.asarray(S).shape)
+    for (t, j), a in np.ndenumerate(c["assign"]):
+        if a >= 0:
+            dS[t, a] = dv[t, j]
+    return c, dict(f=df, w=dw, W2=dW2, b2=db2, z=dz, W1=dW1, b1=db1, y=dy, x=dx, g=dg, b=db, H=dH,
+                   S=dS)
