@@ -471,7 +471,7 @@ int base_gate_backward(const void *dY, const void *F, const void *H, const void 
  *   S         [device] T x E float32 scores, 16-byte aligned
  *   assign    [device] int32 [T, k] out, -1 where fewer than k experts are allowed
  *   scores    [device] float32 [T, k] out, may be NULL: the chosen scores (-inf
- *             where assign is -1)
+ *             where assign is -1: a row without any expert has no softmax)
  *   perm, slots, offsets [device] int32 out, as above
  *   workspace [device] base_topk_workspace_size(T, E, k) bytes, 256-aligned; any
  *             contents at entry. Calls that overlap in time need their own.

@@ -5,7 +5,9 @@ and products on routed rows, with their gradients.
     y, mean, rstd = expert_norm(H, g, b, r.offsets, perm=r.perm, k=2)
     u = expert_linear(y, W1, r.offsets, bias=b1, relu=True)
     f = expert_linear(u, W2, r.offsets, bias=b2)
-    out = combine(f, r.slots, weights=torch.softmax(r.scores, 1), residual=H)
+    some = r.assign[:, :1] >= 0                 # (a softmax over no expert at all is NaN)
+    weights = torch.softmax(r.scores.where(some, 0.0), 1)
+    out = combine(f, r.slots, weights=weights, residual=H)
 
 and back, for an upstream dOut:
 
@@ -16,6 +18,11 @@ and back, for an upstream dOut:
     dy = expert_linear_dx(du, W1, r.offsets)
     dx, dg, db = expert_norm_backward(dy, H, g, mean, rstd, r.offsets, perm=r.perm, k=2)
     dH = combine(dx, r.slots, residual=dOut)
+    ds = weights * (dweights - (weights * dweights).sum(1, keepdim=True))
+    dS = torch.zeros_like(S).scatter_add_(1, r.assign.clamp(min=0).long(), ds)
+
+A token without an expert has scores of -inf, weights that nothing uses and dweights of 0;
+so have the choices that a token has no expert for, and their ds is 0.
 
 Marshals torch tensors into the C calls of include/base.h. Tensors are contiguous
 and on the current device. Work goes to the current stream, or to `stream`, in
