@@ -620,6 +620,16 @@ int base_expert_linear_dw(const void *dy, const void *x, const int32_t *offsets,
 int base_timing_enable(int32_t capacity);
 int base_timing_read(int64_t *launches, double *total_ms);
 
+/*
+ * base_expert_linear_tile - how a product of these sizes (arguments as
+ * base_expert_linear_workspace_size) is computed: tiles of *rows x *cols results, the sum
+ * in *parts parts. On the host; the choice may change between versions, the results only
+ * in their rounding.
+ * Errors: BASE_ERR_INVALID_ARG, BASE_ERR_UNSUPPORTED_DTYPE, BASE_ERR_RANGE.
+ */
+int base_expert_linear_tile(int product, int64_t N, int64_t E, int64_t K, int64_t O, int dtype,
+                            int32_t *rows, int32_t *cols, int32_t *parts);
+
 #ifdef __cplusplus
 }
 #endif

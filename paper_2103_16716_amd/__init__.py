@@ -56,7 +56,7 @@ EXPORTED = ("base_status_string", "base_affinity", "base_affinity_gather",
             "base_sort_by_expert", "base_dispatch", "base_combine", "base_combine_backward",
             "base_expert_norm", "base_expert_norm_workspace_size", "base_expert_norm_backward",
             "base_expert_linear_workspace_size", "base_expert_linear", "base_expert_linear_dx",
-            "base_expert_linear_dw")
+            "base_expert_linear_dw", "base_expert_linear_tile")
 
 
 class AssignOpts(ctypes.Structure):
@@ -153,6 +153,8 @@ def lib() -> ctypes.CDLL:
             fn.argtypes, fn.restype = [i64, i64, i64], sz
         L.base_expert_linear_workspace_size.argtypes = [i32, i64, i64, i64, i64, i32]
         L.base_expert_linear_workspace_size.restype = sz
+        L.base_expert_linear_tile.argtypes = [i32, i64, i64, i64, i64, i32, vp, vp, vp]
+        L.base_expert_linear_tile.restype = i32
         L.base_timing_enable.argtypes = [ctypes.c_int32]
         L.base_timing_enable.restype = i32
         L.base_timing_read.argtypes = [ctypes.POINTER(i64), ctypes.POINTER(ctypes.c_double)]
@@ -517,9 +519,9 @@ def timing_read() -> tuple[int, float]:
 
 
 from .experts import (Routing, combine, combine_backward, dispatch, expert_linear,  # noqa: E402
-                      expert_linear_dw, expert_linear_dx, expert_linear_workspace_size, expert_norm,
-                      expert_norm_backward, expert_norm_workspace_size, sort_by_expert, topk_assign,
-                      topk_workspace_size)
+                      expert_linear_dw, expert_linear_dx, expert_linear_tile,
+                      expert_linear_workspace_size, expert_norm, expert_norm_backward,
+                      expert_norm_workspace_size, sort_by_expert, topk_assign, topk_workspace_size)
 
 __all__ = ["affinity", "assign", "assign_batched", "permute", "permute_batched", "greedy_assign",
            "gate_combine", "gate_combine_batched",
@@ -530,4 +532,5 @@ __all__ = ["affinity", "assign", "assign_batched", "permute", "permute_batched",
            "status_string", "EXPORTED", "Routing", "topk_assign", "topk_workspace_size",
            "sort_by_expert", "dispatch", "combine", "combine_backward", "expert_norm",
            "expert_norm_workspace_size", "expert_norm_backward", "expert_linear",
-           "expert_linear_dx", "expert_linear_dw", "expert_linear_workspace_size"]
+           "expert_linear_dx", "expert_linear_dw", "expert_linear_workspace_size",
+           "expert_linear_tile"]

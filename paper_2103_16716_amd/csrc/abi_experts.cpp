@@ -222,6 +222,16 @@ size_t base_expert_linear_workspace_size(int product, int64_t N, int64_t E, int6
     return base::linear_workspace_size(product, N, E, K, O, dtype == BASE_BF16);
 }
 
+int base_expert_linear_tile(int product, int64_t N, int64_t E, int64_t K, int64_t O, int dtype,
+                            int32_t *rows, int32_t *cols, int32_t *parts) {
+    if (rows == nullptr || cols == nullptr || parts == nullptr || product < BASE_PRODUCT_Y ||
+        product > BASE_PRODUCT_DW)
+        return BASE_ERR_INVALID_ARG;
+    if (const int st = check_linear(N, E, K, O, dtype)) return st;
+    base::linear_tile(product, N, E, K, O, dtype == BASE_BF16, rows, cols, parts);
+    return BASE_OK;
+}
+
 int base_expert_linear(const void *x, const void *w, const void *bias, const void *residual,
                        const int32_t *offsets, void *y, int64_t N, int64_t E, int64_t K, int64_t O,
                        int relu, int dtype, void *workspace, size_t workspace_bytes,

@@ -140,6 +140,8 @@ hipError_t launch_norm_backward(const void *dy, const void *x, const int32_t *pe
 // The experts' products over N routed rows, w [E, O, K] (linear.hip); product: a
 // base_product.
 size_t linear_workspace_size(int product, int64_t N, int64_t E, int64_t K, int64_t O, int bf16);
+void linear_tile(int product, int64_t N, int64_t E, int64_t K, int64_t O, int bf16, int32_t *rows,
+                 int32_t *cols, int32_t *parts);
 hipError_t launch_linear(const void *x, const void *w, const void *bias, const void *residual,
                          const int32_t *offsets, void *y, int64_t N, int64_t E, int64_t K,
                          int64_t O, int relu, int bf16, void *workspace, hipStream_t s);

@@ -1031,18 +1031,13 @@ int parts_of(int form, bool bf16, int64_t N, int64_t E, int64_t K, int64_t O) {
     return best;
 }
 
-template <class In, int kForm>
-hipError_t launch_form(const LinearCall &c, hipStream_t s) {
-    const int64_t avg = c.N / c.E;
-    if (c.parts > 1) {
-        if constexpr (kForm != kTN)
-            return launch_tiles<In, kForm, 64, 64, 2, 2, 3, kInParts>(c, s);
-        else if constexpr (In::kBf16)
-            return launch_tiles<In, kForm, 128, 128, 2, 2, 2, kInParts>(c, s);
-        else
-            return launch_tiles<In, kForm, 64, 128, 2, 2, 2, kInParts>(c, s);
-    }
-    if constexpr (kForm == kTN) {
+constexpr int tile(int rows, int cols) { return rows << 16 | cols; }
+
+// The tile of a call that is in `parts`.
+int tile_of(int form, bool bf16, int64_t N, int64_t E, int64_t K, int64_t O, int64_t parts) {
+    const int64_t avg = N / E;
+    const int64_t cols = form == kNT ? O : K;
+    if (form == kTN) {
         // A tile stores its matrix's part once and multiplies little, so the large tile is for
         // experts with many rows only (128 x 128 and 256 x 256 tiles, us: 64 experts of
         // 4096 x 1024 with 16 rows each 219 and 247, 128 rows 317 and 312, 256 rows 428 and 366;
@@ -1050,41 +1045,59 @@ hipError_t launch_form(const LinearCall &c, hipStream_t s) {
         // started rounds take less time than all smaller tiles (a chunk of one 1.9 and, among
         // others, 0.58; three experts of 5384 x 520, 27587 rows, 261 and 353, 43 of 264 x 1696,
         // 7447 rows, 30 and 53; over 280 calls 1.2 % longer than with the better tile each).
-        if constexpr (!In::kBf16) {
-            return launch_tiles<F32, kTN, 64, 128, 2, 2, 2, kEach>(c, s);
-        } else {
-            const int64_t wide = (int64_t)c.E * ((c.O + 255) / 256) * ((c.K + 255) / 256);
-            const int64_t tiles = (int64_t)c.E * ((c.O + 127) / 128) * ((c.K + 127) / 128);
-            const double rounds = (double)((wide + kUnitsOfDevice - 1) / kUnitsOfDevice);
-            if (avg >= 160 && rounds * 1.9 < (double)tiles / kUnitsOfDevice * 0.58)
-                return launch_tiles<Bf16, kTN, 256, 256, 2, 4, 2, kWide>(c, s);
-            return launch_tiles<Bf16, kTN, 128, 128, 2, 2, 2, kEach>(c, s);
-        }
-    } else if constexpr (!In::kBf16) {
+        if (!bf16) return tile(64, 128);
+        if (parts > 1) return tile(128, 128);
+        const int64_t wide = E * ((O + 255) / 256) * ((K + 255) / 256);
+        const int64_t tiles = E * ((O + 127) / 128) * ((K + 127) / 128);
+        const double rounds = (double)((wide + kUnitsOfDevice - 1) / kUnitsOfDevice);
+        return avg >= 160 && rounds * 1.9 < (double)tiles / kUnitsOfDevice * 0.58 ? tile(256, 256)
+                                                                                  : tile(128, 128);
+    }
+    if (parts > 1) return tile(64, 64);
+    if (!bf16) {
         // Few rows: as much in flight as possible (512 rows of 64 experts, 1024 to 2048: 119 us,
         // 64 x 128 142).
-        if (avg < 32) return launch_tiles<F32, kForm, 32, 128, 1, 4, 3, kEach>(c, s);
-        const int64_t tiles =
-            (c.N / 64 + c.E / 2) * (((kForm == kNT ? c.O : c.K) + 127) / 128);
-        if (tiles < 4 * kUnitsOfDevice)
-            return launch_tiles<F32, kForm, 64, 64, 2, 2, 2, kEach>(c, s);
-        return launch_tiles<F32, kForm, 64, 128, 2, 2, 2, kEach>(c, s);
+        if (avg < 32) return tile(32, 128);
+        const int64_t tiles = (N / 64 + E / 2) * ((cols + 127) / 128);
+        return tiles < 4 * kUnitsOfDevice ? tile(64, 64) : tile(64, 128);
+    }
+    // A few rows: the matrices' bytes count, and what keeps most of them in flight (64 rows
+    // of 64 experts, 1024 to 4096: 58.6 us, 64 x 128 tiles 60.8; of 16, 2048 to 8192: 96 and
+    // 121). By columns a row of 32 x 64 tiles reads too short pieces, but for single rows.
+    if (avg <= (form == kNT ? 16 : 2)) return tile(32, 64);
+    double cost;
+    const TileCost &t = kCosts[form][pick_tile(form, N, E, cols, cost)];
+    return tile(t.bm, t.bn);
+}
+
+template <class In, int kForm>
+hipError_t launch_form(const LinearCall &c, hipStream_t s) {
+    const int shape = tile_of(kForm, In::kBf16, c.N, c.E, c.K, c.O, c.parts);
+    if constexpr (kForm == kTN && In::kBf16) {
+        if (c.parts > 1) return launch_tiles<In, kForm, 128, 128, 2, 2, 2, kInParts>(c, s);
+        if (shape == tile(256, 256))
+            return launch_tiles<In, kForm, 256, 256, 2, 4, 2, kWide>(c, s);
+        return launch_tiles<In, kForm, 128, 128, 2, 2, 2, kEach>(c, s);
+    } else if constexpr (kForm == kTN) {
+        if (c.parts > 1) return launch_tiles<In, kForm, 64, 128, 2, 2, 2, kInParts>(c, s);
+        return launch_tiles<In, kForm, 64, 128, 2, 2, 2, kEach>(c, s);
     } else {
-        // A few rows: the matrices' bytes count, and what keeps most of them in flight (64 rows
-        // of 64 experts, 1024 to 4096: 58.6 us, 64 x 128 tiles 60.8; of 16, 2048 to 8192: 96 and
-        // 121). By columns a row of 32 x 64 tiles reads too short pieces, but for single rows.
-        if constexpr (kForm == kNT)
-            if (avg <= 16)
-                return launch_tiles<Bf16, kForm, 32, 64, 1, 2, 4, kEach>(c, s);
-        if constexpr (kForm == kNN)
-            if (avg <= 2)
-                return launch_tiles<Bf16, kForm, 32, 64, 1, 2, 2, kEach>(c, s);
-        double cost;
-        switch (pick_tile(kForm, c.N, c.E, kForm == kNT ? c.O : c.K, cost)) {
-            case 0: return launch_tiles<Bf16, kForm, 64, 128, 2, 2, 2, kEach>(c, s);
-            case 1: return launch_tiles<Bf16, kForm, 128, 128, 2, 2, 2, kEach>(c, s);
-            case 2: return launch_tiles<Bf16, kForm, 256, 256, 2, 4, 2, kWide>(c, s);
-            default: return launch_tiles<Bf16, kForm, 64, 64, 2, 2, 3, kEach>(c, s);
+        if (c.parts > 1) return launch_tiles<In, kForm, 64, 64, 2, 2, 3, kInParts>(c, s);
+        if constexpr (In::kBf16) {
+            switch (shape) {
+                case tile(32, 64):
+                    return launch_tiles<In, kForm, 32, 64, 1, 2, kForm == kNT ? 4 : 2, kEach>(c, s);
+                case tile(64, 128): return launch_tiles<In, kForm, 64, 128, 2, 2, 2, kEach>(c, s);
+                case tile(128, 128): return launch_tiles<In, kForm, 128, 128, 2, 2, 2, kEach>(c, s);
+                case tile(256, 256): return launch_tiles<In, kForm, 256, 256, 2, 4, 2, kWide>(c, s);
+                default: return launch_tiles<In, kForm, 64, 64, 2, 2, 3, kEach>(c, s);
+            }
+        } else {
+            switch (shape) {
+                case tile(32, 128): return launch_tiles<In, kForm, 32, 128, 1, 4, 3, kEach>(c, s);
+                case tile(64, 128): return launch_tiles<In, kForm, 64, 128, 2, 2, 2, kEach>(c, s);
+                default: return launch_tiles<In, kForm, 64, 64, 2, 2, 2, kEach>(c, s);
+            }
         }
     }
 }
@@ -1152,6 +1165,14 @@ size_t linear_workspace_size(int product, int64_t N, int64_t E, int64_t K, int64
     if (parts == 1) return 0;
     const int64_t n = product == kNT ? N * O : product == kNN ? N * K : E * O * (K + 1);
     return ((size_t)(parts * n) * 4 + 255) / 256 * 256;
+}
+
+void linear_tile(int product, int64_t N, int64_t E, int64_t K, int64_t O, int bf16, int32_t *rows,
+                 int32_t *cols, int32_t *parts) {
+    *parts = parts_of(product, bf16 != 0, N, E, K, O);
+    const int t = tile_of(product, bf16 != 0, N, E, K, O, *parts);
+    *rows = t >> 16;
+    *cols = t & 0xffff;
 }
 
 hipError_t launch_linear(const void *x, const void *w, const void *bias, const void *residual,

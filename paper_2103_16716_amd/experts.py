@@ -33,6 +33,7 @@ unspecified in ones that are not.
 from __future__ import annotations
 
 import contextlib
+import ctypes
 import dataclasses
 
 from . import (BASE_PRODUCT_DW, BASE_PRODUCT_DX, BASE_PRODUCT_Y, _check, _dtype_code, _stream_ptr,
@@ -340,6 +341,16 @@ def expert_norm_backward(dy, x, weight, mean, rstd, offsets=None, perm=None, k: 
 def expert_linear_workspace_size(product: int, N: int, E: int, K: int, O: int, dtype: int) -> int:
     """Bytes for a BASE_PRODUCT_* of these sizes and BASE_* type; 0 for most."""
     return int(lib().base_expert_linear_workspace_size(product, N, E, K, O, dtype))
+
+
+def expert_linear_tile(product: int, N: int, E: int, K: int, O: int, dtype: int):
+    """(rows, columns, parts): the tiles and the parts of the sum that a BASE_PRODUCT_* of
+    these sizes and BASE_* type is computed in (base_expert_linear_tile)."""
+    out = (ctypes.c_int32 * 3)()
+    at = ctypes.addressof(out)
+    _check(lib().base_expert_linear_tile(product, N, E, K, O, dtype, at, at + 4, at + 8),
+           "base_expert_linear_tile")
+    return tuple(out)
 
 
 def _linear_workspace(workspace, product, N, E, K, O, dtype, device):
