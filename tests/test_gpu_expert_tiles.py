@@ -18,6 +18,14 @@ CASES = [
     ("dw", "bf16", 3300, 16, 2040, 1000, (256, 256)),
     ("dw", "bf16", 6500, 40, 1000, 1016, (256, 256)),
     ("dw", "bf16", 1500, 5, 1016, 8184, (256, 256)),
+    # the larger tile of fp32
+    ("y", "f32", 5000, 5, 136, 1640, (64, 128)),
+    ("dx", "f32", 5000, 5, 1640, 136, (64, 128)),
+    # more experts than a wave finds at a time, and than the threads of a block
+    ("y", "bf16", 20000, 100, 72, 2056, (256, 256)),
+    ("y", "bf16", 121000, 600, 72, 1032, (256, 256)),
+    ("dx", "bf16", 26000, 100, 2056, 72, (256, 256)),
+    ("dx", "bf16", 154000, 600, 1032, 72, (256, 256)),
 ]
 
 
