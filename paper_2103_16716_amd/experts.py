@@ -25,7 +25,7 @@ A token without an expert has scores of -inf, weights that nothing uses and dwei
 so have the choices that a token has no expert for, and their ds is 0.
 
 Marshals torch tensors into the C calls of include/base.h. Tensors are contiguous
-and on the current device. Work goes to the current stream, or to `stream`, in
+and, as `stream`, on the current device. Work goes to the current stream, or to `stream`, in
 whose memory pool outputs that are not given are then allocated. Rows that no pair
 has (behind offsets[-1]) are left as they are in outputs that are given, and are
 unspecified in ones that are not.
@@ -93,7 +93,14 @@ def _dims(name, t, n) -> None:
 
 def _on(stream):
     """Where outputs are allocated: the pool of the stream that writes them."""
-    return _current if stream is None else _torch().cuda.stream(stream)
+    if stream is None:
+        return _current
+    torch = _torch()
+    here = torch.cuda.current_device()
+    if stream.device_index != here:
+        raise ValueError(f"stream is on cuda:{stream.device_index}, the current device is "
+                         f"cuda:{here}")
+    return torch.cuda.stream(stream)
 
 
 _current = contextlib.nullcontext()
