@@ -1,8 +1,11 @@
 // Token rows to their experts and back with k experts a token, and the gradient.
 // slots[t k + j] is the routed row of choice j of token t (-1: none), N = T k
-// routed rows. All three kernels go token by token, so that a token's row is read
-// once for its k choices, and sums over choices run in their order, without
-// atomics. An entry of slots outside [0, N) is no row.
+// routed rows. All three kernels go token by token, and sums over choices run in
+// their order, without atomics. dispatch and combine read a token's row once for
+// its k choices. combine_backward goes choice by choice and reads dY[t] again for
+// each: 32768 tokens, two choices, rows of 2048 in bf16 540 MB where 403 would do,
+// 132 us (6.1 TB/s); 8192 tokens of eight 130 us. An entry of slots outside [0, N)
+// is no row.
 #include "common.hpp"
 #include "internal.hpp"
 #include "rows.hpp"
@@ -70,7 +73,8 @@ __global__ __launch_bounds__(kThreads) void combine_kernel(
     }
 }
 
-// A wave per token: dF[r] = w[t, j] dY[t] and dw[t, j] = dY[t] . F[r], r = slots[t, j].
+// A wave per token, one choice after another: dF[r] = w[t, j] dY[t] and dw[t, j] = dY[t] . F[r],
+// r = slots[t, j].
 template <bool BF16>
 __global__ __launch_bounds__(kThreads) void combine_backward_kernel(
     const void *__restrict__ dY, const void *__restrict__ F, const float *__restrict__ w,
