@@ -604,7 +604,9 @@ struct Tiles {
 
     // The tile that is set, then, when next is given, its first loads, which run beside the
     // results' stores. Vector memory operations complete in order, so chunk 0 of the next
-    // tile has landed once no more are in flight than were issued behind it.
+    // tile has landed once no more are in flight than were issued behind it. (What the compiler
+    // keeps in memory, the next Tile and for dW three registers, and the stores of db come on
+    // top of those counted: the wait is then longer than needed, never shorter.)
     template <int X>
     __device__ void compute(const Tile *next) {
         f32x16_t acc[X][TN];
@@ -1056,7 +1058,9 @@ int tile_of(int form, bool bf16, int64_t N, int64_t E, int64_t K, int64_t O, int
     if (parts > 1) return tile(64, 64);
     if (!bf16) {
         // Few rows: as much in flight as possible (512 rows of 64 experts, 1024 to 2048: 119 us,
-        // 64 x 128 142).
+        // 64 x 128 142). The larger tile saves operand reads once there are several to a unit.
+        // Over 120 calls of all sizes 1.9 % longer than with the best of the three tiles each, at
+        // most 23 % (dx of 695 x 248 to 2656, four experts, 19.8 and 16.1 with 32 x 128).
         if (avg < 32) return tile(32, 128);
         const int64_t tiles = (N / 64 + E / 2) * ((cols + 127) / 128);
         return tiles < 4 * kUnitsOfDevice ? tile(64, 64) : tile(64, 128);

@@ -132,9 +132,10 @@ __global__ __launch_bounds__(kBlock<R>) void norm_kernel(
 template <int R>
 constexpr int kRun = 16 * (kBlock<R> / R);
 
-// (Two waves a SIMD, which the compiler else misses by a few registers, and the groups' sums
-// by four columns of a lane next to each other: 32768 rows of 2048 in bf16 87 us; with one wave
-// 104; with the sums in the order of columns, twice the LDS conflicts, 91.)
+// (Two waves a SIMD, which the compiler else misses by a few registers (bf16 rows of 1032 to 2048
+// keep two in memory), and the groups' sums by four columns of a lane next to each other: 32768
+// rows of 2048 in bf16 87 us; with one wave 104; with the sums in the order of columns, twice the
+// LDS conflicts, 91. 12 cycles of conflicts a LDS instruction are left.)
 template <bool BF16, int R, int C>
 __global__ __launch_bounds__(kBlock<R>, 2) void norm_backward_kernel(
     const void *dy, const void *__restrict__ x, const void *__restrict__ g,
@@ -336,7 +337,9 @@ void launch_norm_as(const NormCall &n, hipStream_t s) {
 }
 
 // Threads per row: a wave up to 4 chunks a lane, then a block of four waves, then of eight
-// (1024 threads would leave the gradient half the registers that it needs).
+// (1024 threads would leave the gradient half the registers that it needs; with 512, fp32 rows
+// of more than 8192, eight chunks a thread, keep 42 in memory: 4096 rows of 16384 182 us, 8192
+// of 8192, which have room, 162).
 int row_threads(int64_t ncs) { return ncs <= 256 ? 64 : ncs <= 1024 ? 256 : 512; }
 
 template <bool BF16>

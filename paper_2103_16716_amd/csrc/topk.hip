@@ -179,7 +179,8 @@ __device__ inline void best_of_two_rows(const float *__restrict__ row, const flo
 }
 
 // More choices than the lists hold: k rounds, each of which takes the best of the row and
-// removes it.
+// removes it. Bound by the rounds' chains of maxima over the lanes: 32768 tokens, 16 of 64
+// 21.5 us, 16 of 256 44.4; 8192, 33 of 1000 82.9; 4096, 64 of 2048 149.
 template <int G, int C, class Emit>
 __device__ inline void best_in_rounds(const float *__restrict__ row, int E, int k, int g,
                                       Emit emit) {
@@ -299,7 +300,8 @@ __global__ __launch_bounds__(kThreads) void pair_count_kernel(const int32_t *__r
 }
 
 // A thread per expert (and one for the pairs without): counts become the pairs of earlier
-// blocks, totals the pairs of all.
+// blocks, totals the pairs of all. 14 us for 1024 or 2048 experts of 256 blocks: few waves, each
+// with a chain of loads.
 __global__ __launch_bounds__(64) void pair_scan_kernel(int32_t *__restrict__ counts,
                                                        int32_t *__restrict__ totals, int bins,
                                                        int blocks) {
