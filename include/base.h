@@ -463,6 +463,8 @@ int base_gate_backward(const void *dY, const void *F, const void *H, const void 
  * call waits for the counts, and rows behind offsets[E] are neither read as
  * input that matters nor written.
  * T k < 2^31, E <= 2048, k <= 64 (and k <= E for base_topk_assign).
+ * Outputs and workspaces must not overlap an input or each other, but where an
+ * output may be an input (BASE_ERR_INVALID_ARG).
  *
  * base_topk_assign - the k highest-scoring experts of each token, highest first,
  * the lowest index on ties; then the sort. A score of -inf or NaN is never
@@ -504,8 +506,8 @@ int base_sort_by_expert(const int32_t *assign, int64_t T, int64_t E, int64_t k, 
  *   slots    [device] int32 [T, k]; an entry outside [0, T k) is no row (never
  *            read or written out of bounds). Two pairs with the same row: which
  *            of them writes it is unspecified.
- *   d % 8 == 0, d <= 2^20; rows 16-byte aligned. Outputs must not overlap inputs,
- *   except that out may be residual.
+ *   d % 8 == 0, d <= 2^20; rows 16-byte aligned. out of base_combine may be
+ *   residual.
  * Errors: BASE_ERR_INVALID_ARG, BASE_ERR_UNSUPPORTED_DTYPE, BASE_ERR_RANGE, BASE_ERR_HIP.
  */
 int base_dispatch(const void *in, const float *weights, const int32_t *slots, void *out, int64_t T,
@@ -539,8 +541,8 @@ int base_combine_backward(const void *dY, const void *F, const float *weights,
  *   eps      >= 0, finite
  *   workspace [device] base_expert_norm_workspace_size(N, E, d) bytes, 256-aligned; any
  *            contents at entry. Calls that overlap in time need their own.
- *   N < 2^31, E <= 2048, d % 8 == 0, d <= 16384; matrices 16-byte aligned. y and dx
- *   must not overlap x; dx may be dy or residual.
+ *   N < 2^31, E <= 2048, d % 8 == 0, d <= 16384; matrices 16-byte aligned. dx may be
+ *   dy or residual.
  * Mean, squares about the mean and all sums are fp32, in a fixed order.
  * Errors: BASE_ERR_INVALID_ARG, BASE_ERR_UNSUPPORTED_DTYPE, BASE_ERR_RANGE,
  * BASE_ERR_WORKSPACE, BASE_ERR_HIP.
@@ -573,7 +575,7 @@ int base_expert_norm_backward(const void *dy, const void *x, const int32_t *perm
  *   offsets  [device] int32 [E + 1]. Rows of y and dx outside every range are
  *      left as they are.
  *   N < 2^31, E <= 2048, K % 8 == 0, O % 8 == 0, K, O <= 2^20; 16-byte aligned. y
- *   may be residual and dx may be relu_of; outputs overlap no other input.
+ *   may be residual and dx may be relu_of.
  *   workspace [device] base_expert_linear_workspace_size(product, N, E, K, O, dtype)
  *      bytes, 256-aligned; any contents at entry. Calls that overlap in time need their
  *      own. 0 (then workspace may be NULL) but for calls with few outputs and a long sum,

@@ -3,6 +3,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <initializer_list>
+
 #include "base.h"
 #include "internal.hpp"
 
@@ -26,6 +28,24 @@ bool overlap(const void *a, int64_t an, const void *b, int64_t bn) {
 
 // Overlap other than being the same matrix.
 bool partly(const void *a, const void *b, int64_t n) { return a != b && overlap(a, n, b, n); }
+
+struct Span {
+    const void *at;
+    int64_t bytes;
+};
+
+// Whether an output overlaps an input or another output. (Those that may be an input are
+// looked at with partly, and are not among its `in`.)
+bool clash(std::initializer_list<Span> out, std::initializer_list<Span> in) {
+    for (const Span *a = out.begin(); a != out.end(); ++a) {
+        if (a->bytes == 0) continue;
+        for (const Span *b = a + 1; b != out.end(); ++b)
+            if (b->bytes != 0 && overlap(a->at, a->bytes, b->at, b->bytes)) return true;
+        for (const Span &b : in)
+            if (overlap(a->at, a->bytes, b.at, b.bytes)) return true;
+    }
+    return false;
+}
 
 int64_t size_of(int dtype) { return dtype == BASE_BF16 ? 2 : 4; }
 
@@ -69,10 +89,15 @@ int check_linear(int64_t N, int64_t E, int64_t K, int64_t O, int dtype) {
     return BASE_OK;
 }
 
-bool has_workspace(int product, int64_t N, int64_t E, int64_t K, int64_t O, int dtype,
-                   const void *workspace, size_t bytes) {
-    const size_t need = base::linear_workspace_size(product, N, E, K, O, dtype == BASE_BF16);
-    return need == 0 || (workspace != nullptr && bytes >= need && aligned(workspace, 256));
+// The workspace of a product, as far as it is used, and whether it is there.
+Span used(int product, int64_t N, int64_t E, int64_t K, int64_t O, int dtype,
+          const void *workspace) {
+    return {workspace,
+            (int64_t)base::linear_workspace_size(product, N, E, K, O, dtype == BASE_BF16)};
+}
+bool there(const Span &ws, size_t bytes) {
+    return ws.bytes == 0 ||
+           (ws.at != nullptr && bytes >= (size_t)ws.bytes && aligned(ws.at, 256));
 }
 
 }  // namespace
@@ -98,6 +123,11 @@ int base_topk_assign(const float *S, int64_t T, int64_t E, int64_t k, int32_t *a
     if (workspace == nullptr || workspace_bytes < base::topk_workspace_size(T, E, k) ||
         !aligned(workspace, 256))
         return BASE_ERR_WORKSPACE;
+    const int64_t pairs = T * k * 4;
+    if (clash({{assign, pairs}, {scores, pairs}, {perm, pairs}, {slots, pairs}, {offsets, (E + 1) * 4},
+               {workspace, (int64_t)base::topk_workspace_size(T, E, k)}},
+              {{S, T * E * 4}}))
+        return BASE_ERR_INVALID_ARG;
     return hip_status(base::launch_topk(S, T, E, k, assign, scores, perm, slots, offsets, workspace,
                                         static_cast<hipStream_t>(stream)));
 }
@@ -113,6 +143,11 @@ int base_sort_by_expert(const int32_t *assign, int64_t T, int64_t E, int64_t k, 
     if (workspace == nullptr || workspace_bytes < base::topk_workspace_size(T, E, k) ||
         !aligned(workspace, 256))
         return BASE_ERR_WORKSPACE;
+    const int64_t pairs = T * k * 4;
+    if (clash({{perm, pairs}, {slots, pairs}, {offsets, (E + 1) * 4},
+               {workspace, (int64_t)base::topk_workspace_size(T, E, k)}},
+              {{assign, pairs}}))
+        return BASE_ERR_INVALID_ARG;
     return hip_status(base::launch_topk(nullptr, T, E, k, const_cast<int32_t *>(assign), nullptr,
                                         perm, slots, offsets, workspace,
                                         static_cast<hipStream_t>(stream)));
@@ -125,7 +160,8 @@ int base_dispatch(const void *in, const float *weights, const int32_t *slots, vo
     if (!aligned(in, 16) || !aligned(out, 16) || !aligned(weights, 4) || !aligned(slots, 4))
         return BASE_ERR_INVALID_ARG;
     const int64_t row = d * size_of(dtype);
-    if (overlap(out, T * k * row, in, T * row)) return BASE_ERR_INVALID_ARG;
+    if (clash({{out, T * k * row}}, {{in, T * row}, {weights, T * k * 4}, {slots, T * k * 4}}))
+        return BASE_ERR_INVALID_ARG;
     return hip_status(base::launch_dispatch(in, weights, slots, out, T, k, d, dtype == BASE_BF16,
                                             static_cast<hipStream_t>(stream)));
 }
@@ -138,7 +174,8 @@ int base_combine(const void *F, const float *weights, const int32_t *slots, cons
         !aligned(slots, 4))
         return BASE_ERR_INVALID_ARG;
     const int64_t row = d * size_of(dtype);
-    if (overlap(out, T * row, F, T * k * row) || partly(out, residual, T * row))
+    if (clash({{out, T * row}}, {{F, T * k * row}, {weights, T * k * 4}, {slots, T * k * 4}}) ||
+        partly(out, residual, T * row))
         return BASE_ERR_INVALID_ARG;
     return hip_status(base::launch_combine(F, weights, slots, residual, out, T, k, d,
                                            dtype == BASE_BF16, static_cast<hipStream_t>(stream)));
@@ -155,9 +192,8 @@ int base_combine_backward(const void *dY, const void *F, const float *weights,
         !aligned(slots, 4) || !aligned(dweights, 4))
         return BASE_ERR_INVALID_ARG;
     const int64_t row = d * size_of(dtype);
-    if (overlap(dF, T * k * row, dY, T * row) || overlap(dF, T * k * row, F, T * k * row) ||
-        overlap(dweights, T * k * 4, weights, T * k * 4) ||
-        overlap(dweights, T * k * 4, slots, T * k * 4))
+    if (clash({{dF, T * k * row}, {dweights, T * k * 4}},
+              {{dY, T * row}, {F, T * k * row}, {weights, T * k * 4}, {slots, T * k * 4}}))
         return BASE_ERR_INVALID_ARG;
     return hip_status(base::launch_combine_backward(dY, F, weights, slots, dF, dweights, T, k, d,
                                                     dtype == BASE_BF16,
@@ -176,7 +212,10 @@ int base_expert_norm(const void *x, const int32_t *perm, int64_t x_rows, int64_t
         !aligned(mean, 4) || !aligned(rstd, 4))
         return BASE_ERR_INVALID_ARG;
     const int64_t row = d * size_of(dtype);
-    if (overlap(y, N * row, x, x_rows * row)) return BASE_ERR_INVALID_ARG;
+    if (clash({{y, N * row}, {mean, N * 4}, {rstd, N * 4}},
+              {{x, x_rows * row}, {perm, N * 4}, {weight, E * row}, {bias, E * row},
+               {offsets, (E + 1) * 4}}))
+        return BASE_ERR_INVALID_ARG;
     return hip_status(base::launch_norm(x, perm, x_rows, k, weight, bias, offsets, y, mean, rstd, N,
                                         E, d, eps, dtype == BASE_BF16,
                                         static_cast<hipStream_t>(stream)));
@@ -209,6 +248,13 @@ int base_expert_norm_backward(const void *dy, const void *x, const int32_t *perm
     if (workspace == nullptr || workspace_bytes < base::norm_workspace_size(N, E, d) ||
         !aligned(workspace, 256))
         return BASE_ERR_WORKSPACE;
+    const Span ws = {workspace, (int64_t)base::norm_workspace_size(N, E, d)};
+    const Span dw = {dweight, E * d * 4}, db = {dbias, E * d * 4};
+    if (clash({{dx, N * row}, dw, db, ws},
+              {{x, x_rows * row}, {perm, N * 4}, {weight, E * row}, {mean, N * 4}, {rstd, N * 4},
+               {offsets, (E + 1) * 4}}) ||
+        clash({dw, db, ws}, {{dy, N * row}, {residual, N * row}}))
+        return BASE_ERR_INVALID_ARG;
     return hip_status(base::launch_norm_backward(dy, x, perm, x_rows, k, weight, mean, rstd, offsets,
                                                  residual, dx, dweight, dbias, N, E, d,
                                                  dtype == BASE_BF16, workspace,
@@ -244,11 +290,12 @@ int base_expert_linear(const void *x, const void *w, const void *bias, const voi
         !aligned(y, 16) || !aligned(offsets, 4))
         return BASE_ERR_INVALID_ARG;
     const int64_t sz = size_of(dtype);
-    if (overlap(y, N * O * sz, x, N * K * sz) || overlap(y, N * O * sz, w, E * O * K * sz) ||
-        partly(y, residual, N * O * sz))
+    const Span ws = used(BASE_PRODUCT_Y, N, E, K, O, dtype, workspace);
+    if (clash({{y, N * O * sz}, ws},
+              {{x, N * K * sz}, {w, E * O * K * sz}, {bias, E * O * sz}, {offsets, (E + 1) * 4}}) ||
+        clash({ws}, {{residual, N * O * sz}}) || partly(y, residual, N * O * sz))
         return BASE_ERR_INVALID_ARG;
-    if (!has_workspace(BASE_PRODUCT_Y, N, E, K, O, dtype, workspace, workspace_bytes))
-        return BASE_ERR_WORKSPACE;
+    if (!there(ws, workspace_bytes)) return BASE_ERR_WORKSPACE;
     return hip_status(base::launch_linear(x, w, bias, residual, offsets, y, N, E, K, O, relu,
                                           dtype == BASE_BF16, workspace,
                                           static_cast<hipStream_t>(stream)));
@@ -265,11 +312,12 @@ int base_expert_linear_dx(const void *dy, const void *w, const void *relu_of,
         !aligned(offsets, 4))
         return BASE_ERR_INVALID_ARG;
     const int64_t sz = size_of(dtype);
-    if (overlap(dx, N * K * sz, dy, N * O * sz) || overlap(dx, N * K * sz, w, E * O * K * sz) ||
-        partly(dx, relu_of, N * K * sz))
+    const Span ws = used(BASE_PRODUCT_DX, N, E, K, O, dtype, workspace);
+    if (clash({{dx, N * K * sz}, ws},
+              {{dy, N * O * sz}, {w, E * O * K * sz}, {offsets, (E + 1) * 4}}) ||
+        clash({ws}, {{relu_of, N * K * sz}}) || partly(dx, relu_of, N * K * sz))
         return BASE_ERR_INVALID_ARG;
-    if (!has_workspace(BASE_PRODUCT_DX, N, E, K, O, dtype, workspace, workspace_bytes))
-        return BASE_ERR_WORKSPACE;
+    if (!there(ws, workspace_bytes)) return BASE_ERR_WORKSPACE;
     return hip_status(base::launch_linear_dx(dy, w, relu_of, offsets, dx, N, E, K, O,
                                              dtype == BASE_BF16, workspace,
                                              static_cast<hipStream_t>(stream)));
@@ -285,11 +333,11 @@ int base_expert_linear_dw(const void *dy, const void *x, const int32_t *offsets,
         !aligned(offsets, 4))
         return BASE_ERR_INVALID_ARG;
     const int64_t sz = size_of(dtype);
-    if (overlap(dw, E * O * K * 4, dy, N * O * sz) || overlap(dw, E * O * K * 4, x, N * K * sz) ||
-        overlap(dw, E * O * K * 4, db, E * O * 4))
+    const Span ws = used(BASE_PRODUCT_DW, N, E, K, O, dtype, workspace);
+    if (clash({{dw, E * O * K * 4}, {db, E * O * 4}, ws},
+              {{dy, N * O * sz}, {x, N * K * sz}, {offsets, (E + 1) * 4}}))
         return BASE_ERR_INVALID_ARG;
-    if (!has_workspace(BASE_PRODUCT_DW, N, E, K, O, dtype, workspace, workspace_bytes))
-        return BASE_ERR_WORKSPACE;
+    if (!there(ws, workspace_bytes)) return BASE_ERR_WORKSPACE;
     return hip_status(base::launch_linear_dw(dy, x, offsets, dw, db, N, E, K, O,
                                              dtype == BASE_BF16, workspace,
                                              static_cast<hipStream_t>(stream)));
