@@ -1,5 +1,5 @@
-"""k experts a token and the experts themselves: routing, row moves, layer norm
-and products on routed rows, with their gradients.
+"""k experts a token and the experts themselves: routing; row moves, layer norm
+and products on routed rows, and their gradients.
 
     r = topk_assign(S, 2)                       # 2 experts a token, rows by expert
     y, mean, rstd = expert_norm(H, g, b, r.offsets, perm=r.perm, k=2)
